@@ -41,6 +41,7 @@ extern "C" {
 typedef struct sd_ctx sd_ctx; /* opaque */
 
 enum { SD_F32 = 0, SD_BF16 = 1 };                 /* storage type of weight matrices and KV cache        */
+enum { SD_MX4 = 2 };                              /* panels of MXFP4 (sd_mx4_*)                          */
 enum { SD_GREEDY = 0, SD_SAMPLE = 1 };            /* decoding mode                                       */
 enum { SD_LOGITS_DRAFT = 0, SD_LOGITS_VERIFY = 1 };
 enum { SD_SKIP_ATTN = 1, SD_SKIP_FFN = 2 };       /* skip-mask bits per layer (3 = whole layer)          */
@@ -279,6 +280,55 @@ int sd_fit_prune_mask(const double *t_attn, const double *t_ffn, int32_t n_layer
  * smallest t_ffn, ranked separately.  All HOST; errors as above. */
 int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_layers, double ratio_attn, double ratio_ffn,
                            uint8_t *mask_out);
+
+/* ---- The output head's way to a token: MXFP4 matrices and rules on logits --------------------------------------------
+ * Operators of their own, without a context: they enqueue on hip_stream (a stream of the current device) and return, wait
+ * for nothing, need no workspace and can be captured into a graph.  Pointers are DEVICE unless marked.  Errors: SD_EINVAL
+ * (null or misaligned pointer, size, type), SD_ENOMEM (a buffer of panels is too small), SD_EHIP.
+ *
+ * MXFP4 (SD_MX4): blocks of 32 neighbouring columns of a row share a scale 2^(e - 127), e one byte, and hold 4-bit values
+ * of the grid 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign.  A matrix of rows x cols lies in panels of 64 rows x 128 columns,
+ * [ceil(rows / 64)][ceil(cols / 128)][4352 bytes]: 4096 bytes of codes -- row 16 t + r, block b of the panel at
+ * ((t * 4 + b) * 16 + r) * 16, column 2 i of the block in the low four bits of byte i, column 2 i + 1 in the high four --,
+ * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes.  A scale byte 255 marks a block of NaN.
+ * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned. */
+size_t sd_mx4_bytes(int32_t rows, int32_t cols);
+/* Quantise rows (dtype SD_F32 or SD_BF16, ld >= cols elements apart, any alignment of their elements): the scale of a block
+ * is 2^(floor(log2 max|x|) - 2), at least 2^-126, and every value is rounded to the nearest grid value (ties to the even
+ * code, 6 at most).  A block that holds an infinity or a NaN becomes NaN throughout.  q: sd_mx4_bytes(rows, cols) bytes. */
+int sd_mx4_quantize(const void *x, int dtype, int64_t ld, int32_t rows, int32_t cols, void *q, size_t q_bytes,
+                    void *hip_stream);
+/* The values that panels stand for, as rows of dtype SD_F32 or SD_BF16 (both exact). */
+int sd_mx4_dequantize(const void *q, size_t q_bytes, int32_t rows, int32_t cols, void *x, int dtype, int64_t ld,
+                      void *hip_stream);
+/* y[M][N] = x w^T with w [N][K] in panels.  x: rows of SD_F32 (multiplied exactly, as three bfloat16 pieces) or SD_BF16, ldx
+ * elements apart, or SD_MX4: panels of [M][K], ldx their size in bytes.  Sums are float32; y: rows of y_dtype SD_F32 or
+ * SD_BF16, rounded once, ldy >= N elements apart.  gain: NULL, or float32 [K] with float32 x: the rows are RMS-normalised
+ * first, x^ = x * gain / sqrt(mean(x^2) + eps), as in front of an output head.  The same arguments give the same bits. */
+int sd_mx4_matmul(const void *w, size_t w_bytes, int32_t N, int32_t K, const void *x, int x_dtype, int64_t ldx, int32_t M,
+                  const float *gain, float eps, void *y, int y_dtype, int64_t ldy, void *hip_stream);
+
+/* Rules on logits.  With n the occurrences of token j in the row's history, the logit z of token j becomes, in this order,
+ *   n > 0:  z / repetition if z > 0, z * repetition otherwise;  then  z - frequency * n - presence;
+ *   always: z + bias[j];  -inf if j is not allowed.
+ * Every operation is rounded to float32; bfloat16 logits are rounded once, at the end. */
+typedef struct {
+    float repetition;            /* > 0, 1 = none                                                           */
+    float presence, frequency;   /* finite, 0 = none                                                        */
+    const float *bias;           /* DEVICE float32 [vocab], or NULL                                         */
+    const uint32_t *allowed;     /* DEVICE [n_masks][ceil(vocab / 32)], bit j % 32 of word j / 32 allows    */
+                                 /* token j; or NULL                                                        */
+    int32_t n_masks;             /* >= 1 where allowed is given                                             */
+} sd_rules;
+/* rows of logits z (dtype SD_F32 or SD_BF16, ld >= vocab elements apart, any alignment of their elements) to out (the same
+ * type; out == z with ld_out == ld works in place, other overlaps do not).  rules: HOST.  The history of row i is
+ * tokens[begin[i] .. end[i]), cut to 0 .. n_tokens: ranges may overlap, so the rows of one step can share a history; token
+ * ids outside the vocabulary count for nothing, an empty range is no history.  tokens, begin and end are read only if some
+ * penalty is set.  mask_row[i]: the mask of row i, a value outside 0 .. n_masks - 1 leaves the row unmasked; NULL: mask i,
+ * or mask 0 for all if there is one.  A mask that allows nothing leaves a row of -inf. */
+int sd_logits_rules(const void *z, int dtype, int64_t ld, int32_t rows, int32_t vocab, const sd_rules *rules,
+                    const int32_t *tokens, int64_t n_tokens, const int64_t *begin, const int64_t *end,
+                    const int32_t *mask_row, void *out, int64_t ld_out, void *hip_stream);
 
 #ifdef __cplusplus
 }

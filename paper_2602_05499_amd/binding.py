@@ -9,7 +9,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
-SD_F32, SD_BF16 = 0, 1
+SD_F32, SD_BF16, SD_MX4 = 0, 1, 2
 SD_GREEDY, SD_SAMPLE = 0, 1
 SD_LOGITS_DRAFT, SD_LOGITS_VERIFY = 0, 1
 SD_OK, SD_EINVAL, SD_ECAPACITY, SD_ESTATE, SD_EHIP, SD_ENOMEM, SD_ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
@@ -22,6 +22,7 @@ EXPORTED_SYMBOLS = (
     "sd_accept", "sd_rollback", "sd_decode", "sd_set_pending", "sd_set_draft", "sd_read", "sd_dump_logits",
     "sd_dump_draft", "sd_keep_logits", "sd_phase_trace", "sd_phase_trace_read", "sd_set_spin_limit", "sd_set_turn_span", "sd_set_prefill_mode", "sd_tiled_weights_bytes", "sd_set_tiled_weights", "sd_guard_read", "sd_guard_host_buffer", "sd_sync", "sd_last_hip_error", "sd_free", "sd_strerror",
     "sd_fit_workspace_bytes", "sd_fit_scores", "sd_fit_prune_mask", "sd_fit_prune_sublayers",
+    "sd_mx4_bytes", "sd_mx4_quantize", "sd_mx4_dequantize", "sd_mx4_matmul", "sd_logits_rules",
 )
 
 
@@ -44,6 +45,11 @@ class SdWeights(ctypes.Structure):
 class SdStats(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("steps", "drafted", "accepted", "examined", "committed")]
     _fields_ += [(n, ctypes.c_int32) for n in ("cache_len", "t_last", "last_n", "last_k")]
+
+
+class SdRules(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float),
+                ("bias", ctypes.c_void_p), ("allowed", ctypes.c_void_p), ("n_masks", ctypes.c_int32)]
 
 
 class SdError(RuntimeError):
@@ -116,6 +122,13 @@ def load_library():
     lib.sd_free.restype = None
     lib.sd_strerror.argtypes = [ctypes.c_int]
     lib.sd_strerror.restype = ctypes.c_char_p
+    sz, i64, ci = ctypes.c_size_t, ctypes.c_int64, ctypes.c_int
+    lib.sd_mx4_bytes.restype = sz
+    lib.sd_mx4_bytes.argtypes = [i32, i32]
+    lib.sd_mx4_quantize.argtypes = [vp, ci, i64, i32, i32, vp, sz, vp]
+    lib.sd_mx4_dequantize.argtypes = [vp, sz, i32, i32, vp, ci, i64, vp]
+    lib.sd_mx4_matmul.argtypes = [vp, sz, i32, i32, vp, ci, i64, i32, vp, ctypes.c_float, vp, ci, i64, vp]
+    lib.sd_logits_rules.argtypes = [vp, ci, i64, i32, i32, ctypes.POINTER(SdRules), vp, i64, vp, vp, vp, vp, i64, vp]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int and name not in ("sd_kv_bytes", "sd_workspace_bytes", "sd_tiled_weights_bytes"):
@@ -261,6 +274,30 @@ def sd_fit_prune_sublayers(t_attn, t_ffn, ratio_attn, ratio_ffn):
     rc = load_library().sd_fit_prune_sublayers(ta.ctypes.data_as(f64p), tf.ctypes.data_as(f64p), len(ta), float(ratio_attn),
                                                float(ratio_ffn), mask.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)))
     return rc, mask
+
+
+# the operators without a context: *_ptr and stream are integer device addresses / stream handles (None = NULL)
+def sd_mx4_bytes(rows, cols):
+    return load_library().sd_mx4_bytes(rows, cols)
+
+
+def sd_mx4_quantize(x_ptr, dtype, ld, rows, cols, q_ptr, q_bytes, stream):
+    return load_library().sd_mx4_quantize(x_ptr, dtype, ld, rows, cols, q_ptr, q_bytes, stream)
+
+
+def sd_mx4_dequantize(q_ptr, q_bytes, rows, cols, x_ptr, dtype, ld, stream):
+    return load_library().sd_mx4_dequantize(q_ptr, q_bytes, rows, cols, x_ptr, dtype, ld, stream)
+
+
+def sd_mx4_matmul(w_ptr, w_bytes, N, K, x_ptr, x_dtype, ldx, M, gain_ptr, eps, y_ptr, y_dtype, ldy, stream):
+    return load_library().sd_mx4_matmul(w_ptr, w_bytes, N, K, x_ptr, x_dtype, ldx, M, gain_ptr, eps, y_ptr, y_dtype, ldy, stream)
+
+
+def sd_logits_rules(z_ptr, dtype, ld, rows, vocab, rules, tokens_ptr, n_tokens, begin_ptr, end_ptr, mask_row_ptr, out_ptr,
+                    ld_out, stream):
+    """rules: SdRules."""
+    return load_library().sd_logits_rules(z_ptr, dtype, ld, rows, vocab, ctypes.byref(rules) if rules is not None else None,
+                                          tokens_ptr, n_tokens, begin_ptr, end_ptr, mask_row_ptr, out_ptr, ld_out, stream)
 
 
 def sd_set_prefill_mode(ctx, mode):

@@ -1,0 +1,367 @@
+// MXFP4 kernels: quantisation to panels, reading back, and the product of rows with a matrix in panels.
+#pragma once
+#include "sdfp_common.hip.h"
+#include "sdfp_mx4.h"
+
+namespace sdfp {
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // 16 bytes at any element's address
+typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+template <int XT> struct Mx4In;     // storage of unquantised rows; VE elements fill 16 bytes
+template <> struct Mx4In<MX4_X_F32> {
+    typedef float T;
+    static constexpr int VE = 4;
+    static __device__ __forceinline__ float val(float v) { return v; }
+    static __device__ __forceinline__ void unpack(const u32x4& r, float (&v)[4]) {
+        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[4]) {
+        return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+    static __device__ __forceinline__ float out(float v) { return v; }
+};
+template <> struct Mx4In<MX4_X_BF16> {
+    typedef bf16_t T;
+    static constexpr int VE = 8;
+    static __device__ __forceinline__ float val(bf16_t v) { return bf16_to_f32(v); }
+    static __device__ __forceinline__ void unpack(const u32x4& r, float (&v)[8]) { ST<bf16_t>::unpack(r, v); }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[8]) {
+        return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    }
+    static __device__ __forceinline__ bf16_t out(float v) { return (bf16_t)pack_bf16(v, v); }
+};
+
+// VE elements of a row from column k on, zeros past its end; full: all of them exist
+template <int XT>
+__device__ __forceinline__ u32x4 mx4_load(const typename Mx4In<XT>::T* row, int64_t k, int cols, bool full) {
+    if (full) return *reinterpret_cast<const SDFP_GLOBAL u32x4_any*>(as_global(row + k));
+    u32x4 r{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < Mx4In<XT>::VE; ++i)
+        if (k + i < cols) {
+            if (XT == MX4_X_F32) r[i] = reinterpret_cast<const unsigned*>(row)[k + i];
+            else r[i / 2] |= (unsigned)reinterpret_cast<const bf16_t*>(row)[k + i] << (16 * (i % 2));
+        }
+    return r;
+}
+
+// ---- quantisation.  A block of 32 columns shares the scale s = 2^(floor(log2 max|x|) - 2), at least 2^-126, so that the
+// largest magnitude lands in [4, 8) of the grid {0, .5, 1, 1.5, 2, 3, 4, 6}; values are rounded to nearest, ties to the even
+// code, and saturate at 6.  |x| / s is exact (a power of two; what underflows rounds to zero either way).  A block with an
+// infinity or a NaN gets the scale 255, NaN throughout.  One workgroup per panel: a block is held by 32 / VE neighbouring
+// lanes, which exchange the maximum of their bit patterns (as integers: NaN above infinity above all finite magnitudes); the
+// panel is put together in LDS and leaves as 4352 contiguous bytes.  Bound by the read of the rows.
+template <int XT>
+__global__ __launch_bounds__(256) void k_mx4_quantize(const void* __restrict__ x_, int64_t ld, int rows, int cols, char* __restrict__ q) {
+    typedef typename Mx4In<XT>::T T;
+    constexpr int VE = Mx4In<XT>::VE, PER_ROW = MX4_COLS / VE, PER_BLOCK = MX4_BLOCK / VE, RP = 256 / PER_ROW, NP = MX4_ROWS / RP;
+    __shared__ __attribute__((aligned(16))) char sh[MX4_PANEL_BYTES];
+    const int kps = (cols + MX4_COLS - 1) / MX4_COLS, kp = blockIdx.x % kps, tid = threadIdx.x, lc = tid % PER_ROW;
+    const int64_t row0 = (int64_t)(blockIdx.x / kps) * MX4_ROWS;
+    const int k = kp * MX4_COLS + lc * VE;
+    const bool full = kp * (int64_t)MX4_COLS + MX4_COLS <= cols;
+    const T* x = reinterpret_cast<const T*>(x_);
+    u32x4 raw[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int64_t row = row0 + i * RP + tid / PER_ROW;
+        raw[i] = row < rows ? mx4_load<XT>(x + row * ld, k, cols, full) : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int r = i * RP + tid / PER_ROW, t = r / 16, b = lc / PER_BLOCK;
+        float v[VE];
+        Mx4In<XT>::unpack(raw[i], v);
+        unsigned amax = 0;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) amax = max(amax, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+#pragma unroll
+        for (int o = 1; o < PER_BLOCK; o <<= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, o));
+        const int ex = (int)(amax >> 23);                        // biased exponent of the largest magnitude
+        const int sc = ex == 255 ? 255 : max(ex - 2, 1);
+        const float inv = ex == 255 ? 0.f : __uint_as_float((unsigned)(254 - sc) << 23);   // 1 / s
+        unsigned w = 0;
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float a = ex == 255 ? 0.f : v[e] * inv, c = ex == 255 ? 0.f : v[e + 1] * inv;
+            if (e == 0) w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, c, 1.0f, 0);
+            if (e == 2) w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, c, 1.0f, 1);
+            if (e == 4) w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, c, 1.0f, 2);
+            if (e == 6) w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, c, 1.0f, 3);
+        }
+        char* code = sh + ((t * 4 + b) * 16 + r % 16) * 16 + (lc % PER_BLOCK) * (VE / 2);
+        if (VE == 8) *reinterpret_cast<unsigned*>(code) = w;
+        else *reinterpret_cast<unsigned short*>(code) = (unsigned short)w;
+        if (lc % PER_BLOCK == 0) sh[MX4_CODE_BYTES + (b * 16 + r % 16) * 4 + t] = (char)sc;
+    }
+    __syncthreads();
+    char* dst = q + (size_t)blockIdx.x * MX4_PANEL_BYTES;
+    for (int o = tid * 16; o < MX4_PANEL_BYTES; o += 256 * 16)
+        *reinterpret_cast<u32x4*>(dst + o) = *reinterpret_cast<const u32x4*>(sh + o);
+}
+
+// the scale 2^(e - 127) of a scale byte as a float32; 0 stands for 2^-127, 255 for NaN
+__device__ __forceinline__ float mx4_scale(unsigned e) {
+    return e == 255u ? __uint_as_float(0x7FC00000u) : e == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(e << 23);
+}
+
+// ---- reading back: the values that panels stand for, as float32 or bfloat16 rows.  One workgroup per panel.
+template <int XT>
+__global__ __launch_bounds__(256) void k_mx4_dequantize(const char* __restrict__ q, int rows, int cols, void* __restrict__ x_, int64_t ld) {
+    typedef typename Mx4In<XT>::T T;
+    constexpr int VE = Mx4In<XT>::VE, PER_ROW = MX4_COLS / VE, PER_BLOCK = MX4_BLOCK / VE, RP = 256 / PER_ROW, NP = MX4_ROWS / RP;
+    __shared__ __attribute__((aligned(16))) char sh[MX4_PANEL_BYTES];
+    const int kps = (cols + MX4_COLS - 1) / MX4_COLS, kp = blockIdx.x % kps, tid = threadIdx.x, lc = tid % PER_ROW;
+    const int64_t row0 = (int64_t)(blockIdx.x / kps) * MX4_ROWS;
+    const int k = kp * MX4_COLS + lc * VE, b = lc / PER_BLOCK;
+    const bool full = kp * (int64_t)MX4_COLS + MX4_COLS <= cols;
+    const char* src = q + (size_t)blockIdx.x * MX4_PANEL_BYTES;
+    for (int o = tid * 16; o < MX4_PANEL_BYTES; o += 256 * 16)
+        *reinterpret_cast<u32x4*>(sh + o) = *reinterpret_cast<const u32x4*>(src + o);
+    __syncthreads();
+    T* x = reinterpret_cast<T*>(x_);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int r = i * RP + tid / PER_ROW, t = r / 16;
+        const int64_t row = row0 + r;
+        if (row >= rows) continue;
+        const char* code = sh + ((t * 4 + b) * 16 + r % 16) * 16 + (lc % PER_BLOCK) * (VE / 2);
+        const unsigned w = VE == 8 ? *reinterpret_cast<const unsigned*>(code) : *reinterpret_cast<const unsigned short*>(code);
+        const float s = mx4_scale((unsigned char)sh[MX4_CODE_BYTES + (b * 16 + r % 16) * 4 + t]);
+        float v[VE];
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            f32x2_t f = {0.f, 0.f};
+            if (e == 0) f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+            if (e == 2) f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+            if (e == 4) f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+            if (e == 6) f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+            v[e] = f.x * s; v[e + 1] = f.y * s;
+        }
+        T* to = x + row * ld + k;
+        if (full) {
+            *reinterpret_cast<u32x4_any*>(to) = Mx4In<XT>::pack(v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VE; ++e)
+                if (k + e < cols) to[e] = Mx4In<XT>::out(v[e]);
+        }
+    }
+}
+
+// A float32 value as three bfloat16 pieces by truncation, x = x0 + x1 + x2 exactly (8 bits of the significand each; what is
+// below the smallest bfloat16 is lost); the pieces' bits lie in the upper halves.  Truncation keeps the first piece of a large
+// finite value finite; an infinity is its first piece alone, a NaN stays NaN.
+__device__ __forceinline__ void trunc3(float x, unsigned (&p)[3]) {
+    p[0] = __float_as_uint(x) & 0xFFFF0000u;
+    float r = sub_rn(x, __uint_as_float(p[0]));
+    if (p[0] << 1 == 0xFF000000u) r = __float_as_uint(x) == p[0] ? 0.f : x;   // infinity; NaN whose payload was cut off
+    p[1] = __float_as_uint(r) & 0xFFFF0000u;
+    p[2] = __float_as_uint(sub_rn(r, __uint_as_float(p[1]))) & 0xFFFF0000u;
+    if (x != x) p[0] = 0x7FC00000u;
+}
+
+// 8 values of a block -- the codes of one word -- as a bfloat16 matrix-core operand, scale applied (exact)
+__device__ __forceinline__ bf16x8 mx4_decode(unsigned w, float s) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1),
+                   c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+    return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+__device__ __forceinline__ f32x4 mx4_mfma(const u32x4& a, int sa, const u32x4& b, int sb, const f32x4& c) {
+    const i32x8 A = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, B = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, 0, sa, 0, sb);
+}
+// the high bit of every byte of s that is 255
+__device__ __forceinline__ unsigned mx4_nan_bytes(unsigned s) { return ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u; }
+
+// four neighbouring outputs n .. n + 3 of row m (those that exist)
+__device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_t n, const float (&v)[4]) {
+    const bool whole = n + 4 <= a.N;
+    if (a.y_type == MX4_X_F32) {
+        float* y = (float*)a.y + m * a.ldy + n;
+        if (whole) *reinterpret_cast<u32x4_any*>(y) = Mx4In<MX4_X_F32>::pack(v);
+        else for (int i = 0; n + i < a.N; ++i) y[i] = v[i];
+    } else {
+        bf16_t* y = (bf16_t*)a.y + m * a.ldy + n;
+        if (whole) *reinterpret_cast<u32x2_any*>(y) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        else for (int i = 0; n + i < a.N; ++i) y[i] = (bf16_t)pack_bf16(v[i], v[i]);
+    }
+}
+
+// ---- product of a few rows: bound by the read of the panels.  A workgroup computes one panel's 64 outputs for 16 rows of x,
+// its waves split the reduction dimension by panels and add their sums in wave order at the end.  The panel's codes go from
+// memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies the
+// 8 values of word j), x into the B operand with the same permutation of columns.  float32 x runs as three exact bfloat16
+// pieces, in MXFP4 as it is on the scaled 4-bit instruction.  MP: rows of x that are staged (a power of two; lanes of the
+// operand past them read the same values again, their columns are not stored).
+// W: waves of the workgroup, as many as the staged rows leave room for in 64 KB of LDS.
+constexpr int mx4_rows_waves(int xt, int mp) { return xt == MX4_X_F32 && mp == 16 ? 4 : 8; }
+template <int XT, int MP>
+__global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Product a) {
+    constexpr int W = mx4_rows_waves(XT, MP);
+    constexpr int NPC = XT == MX4_X_F32 ? 3 : 1;
+    constexpr int STAGE = XT == MX4_X_MX4 ? 0 : NPC * 16 * MP * 16;          // bytes of a wave's staged panel of x
+    constexpr int RED = W * 4 * 64 * 16;
+    __shared__ __attribute__((aligned(16))) char sh[W * STAGE > RED ? W * STAGE : RED];
+    __shared__ float s_sq[W][16];
+    __shared__ unsigned s_bad_n[MX4_ROWS], s_bad_m[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS;
+    const int my = (a.M + 15) / 16, panel = blockIdx.x / my;
+    const int64_t m0 = (int64_t)(blockIdx.x % my) * 16;
+    const char* wp = a.w + (size_t)panel * kps * MX4_PANEL_BYTES;
+    if (tid < MX4_ROWS) s_bad_n[tid] = 0;
+    if (tid < 16) s_bad_m[tid] = 0;
+    __syncthreads();
+
+    f32x4 acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    unsigned bad = 0, bad_x = 0;
+    constexpr int VE = XT == MX4_X_F32 ? 4 : 8;
+    constexpr int PER_ROW = MX4_COLS / VE;                                   // lanes per row of a staged panel
+    constexpr int NL = XT == MX4_X_MX4 ? 1 : (MP * PER_ROW + 63) / 64;       // loads per lane
+    float sq[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) sq[i] = 0.f;
+    char* stage = sh + wave * STAGE;
+
+    struct Load { u32x4 code[4]; unsigned scale; u32x4 x[NL]; u32x4 gain; };
+    auto fetch = [&](int kp, Load& L, bool tail) {
+        const char* p = wp + (size_t)kp * MX4_PANEL_BYTES + lane * 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) L.code[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(p + t * MX4_TILE_BYTES));
+        L.scale = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(p + MX4_CODE_BYTES - lane * 12));
+        if constexpr (XT == MX4_X_MX4) {
+            const char* xp = (const char*)a.x + ((size_t)(m0 / MX4_ROWS) * kps + kp) * MX4_PANEL_BYTES;
+            const int t = (int)(m0 / 16) & 3;
+            L.x[0] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(xp + t * MX4_TILE_BYTES + lane * 16));
+            L.gain.x = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(xp + MX4_CODE_BYTES + lane * 4)) >> (8 * t) & 255u;
+        } else {
+            typedef typename Mx4In<XT>::T T;
+            const int k = kp * MX4_COLS + (lane % PER_ROW) * VE;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int64_t row = min(m0 + min((i * 64 + lane) / PER_ROW, MP - 1), (int64_t)a.M - 1);
+                L.x[i] = mx4_load<XT>((const T*)a.x + row * a.ldx, k, a.K, !tail);
+            }
+            if constexpr (XT == MX4_X_F32)
+                if (a.gain) L.gain = mx4_load<XT>(a.gain, k, a.K, !tail);
+        }
+    };
+    auto multiply = [&](const Load& L) {
+        bad |= mx4_nan_bytes(L.scale);
+        if constexpr (XT == MX4_X_MX4) {
+            bad_x |= L.gain.x == 255u;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] = mx4_mfma(L.code[t], (int)(L.scale >> (8 * t)), L.x[0], (int)L.gain.x, acc[t]);
+        } else {
+            // x of this panel into LDS: piece p, sub-step j, block b, row m at (((p * 4 + j) * 4 + b) * MP + m) * 16
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int m = (i * 64 + lane) / PER_ROW, cc = (lane % PER_ROW) * VE, b = cc / 32, j = cc % 32 / 8;
+                char* to = stage + ((j * 4 + b) * MP + m) * 16;
+                if constexpr (XT == MX4_X_F32) {
+                    float v[4], gn[4];
+                    Mx4In<XT>::unpack(L.x[i], v);
+                    if (a.gain) {
+                        Mx4In<XT>::unpack(L.gain, gn);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { sq[i] = fmaf(v[e], v[e], sq[i]); v[e] *= gn[e]; }
+                    }
+                    unsigned pc[4][3];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) trunc3(v[e], pc[e]);
+                    if (m < MP)
+#pragma unroll
+                        for (int p = 0; p < 3; ++p)
+                            *reinterpret_cast<u32x2*>(to + p * 16 * MP * 16 + cc % 8 * 2) =
+                                u32x2{pc[0][p] >> 16 | pc[1][p], pc[2][p] >> 16 | pc[3][p]};
+                } else {
+                    if (m < MP) *reinterpret_cast<u32x4*>(to) = L.x[i];
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+            float s[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const unsigned e = L.scale >> (8 * t) & 255u;
+                s[t] = __uint_as_float(e == 0u ? 0x00400000u : e << 23);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 xb[NPC];
+#pragma unroll
+                for (int p = 0; p < NPC; ++p)
+                    xb[p] = *reinterpret_cast<const bf16x8*>(stage + (((p * 4 + j) * 4 + g) * MP + (c16 & (MP - 1))) * 16);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const bf16x8 wb = mx4_decode(L.code[t][j], s[t]);
+#pragma unroll
+                    for (int p = 0; p < NPC; ++p) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[p], acc[t], 0, 0, 0);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+
+    const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
+    Load cur, nxt;
+    if (wave < full) fetch(wave, cur, false);
+    for (int kp = wave; kp < full; kp += W) {
+        if (kp + W < full) fetch(kp + W, nxt, false);
+        multiply(cur);
+        cur = nxt;
+    }
+    if (full < kps && full % W == wave) { fetch(full, cur, true); multiply(cur); }
+
+    // sums of the waves, in wave order
+    if (bad)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (bad >> (8 * t) & 128u) s_bad_n[t * 16 + c16] = 1u;
+    if (bad_x) s_bad_m[c16] = 1u;
+    if constexpr (XT == MX4_X_F32)
+        if (a.gain)
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                float v = sq[i];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o);
+                const int m = (i * 64 + lane) / PER_ROW;
+                if (lane % 32 == 0 && m < 16) s_sq[wave][m] = v;
+            }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(sh + ((wave * 4 + t) * 64 + lane) * 16) = acc[t];
+    __syncthreads();
+    if (tid >= 256) return;
+    f32x4 y = *reinterpret_cast<const f32x4*>(sh + tid * 16);
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+        const f32x4 o = *reinterpret_cast<const f32x4*>(sh + (w * 256 + tid) * 16);
+        y.x += o.x; y.y += o.y; y.z += o.z; y.w += o.w;
+    }
+    const int64_t m = m0 + c16;
+    const int nr = (tid >> 6) * 16 + g * 4;
+    const int64_t n = (int64_t)panel * MX4_ROWS + nr;
+    if (m >= a.M || n >= a.N) return;
+    float v[4] = {y.x, y.y, y.z, y.w};
+    if constexpr (XT == MX4_X_F32)
+        if (a.gain) {
+            float ss = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) ss += s_sq[w][c16];
+            const float rs = rms_recip(ss, a.K, a.eps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= rs;
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (s_bad_n[nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
+    mx4_store(a, m, n, v);
+}
+
+}  // namespace sdfp

@@ -1,0 +1,46 @@
+// Entry point of the rules on rows of logits (include/sdfp.h): argument checks and the launch.
+#include "sdfp_rules_args.h"
+#include "sdfp.h"
+
+using namespace sdfp;
+
+namespace {
+
+// The shortest chunk, unless a longer one still gives every compute unit two workgroups.
+template <typename T>
+hipError_t launch(const RulesRows& a, hipStream_t s) {
+    auto chunks = [&](int ch) { return (int64_t)a.rows * ((a.vocab + ch - 1) / ch); };
+    if (chunks(1024) > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (chunks(8192) >= 512) hipLaunchKernelGGL((k_logits_rules<T, 8192>), dim3((unsigned)chunks(8192)), dim3(RULES_THREADS), 0, s, a);
+    else if (chunks(4096) >= 512) hipLaunchKernelGGL((k_logits_rules<T, 4096>), dim3((unsigned)chunks(4096)), dim3(RULES_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((k_logits_rules<T, 1024>), dim3((unsigned)chunks(1024)), dim3(RULES_THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+extern "C" int sd_logits_rules(const void* z, int dtype, int64_t ld, int32_t rows, int32_t vocab, const sd_rules* rules,
+                               const int32_t* tokens, int64_t n_tokens, const int64_t* begin, const int64_t* end,
+                               const int32_t* mask_row, void* out, int64_t ld_out, void* hip_stream) {
+    if (!z || !out || !rules || rows < 1 || vocab < 1 || vocab > INT32_MAX - 8192 || ld < vocab || ld_out < vocab) return SD_EINVAL;
+    if (dtype != SD_F32 && dtype != SD_BF16) return SD_EINVAL;
+    const uintptr_t es = dtype == SD_F32 ? 4 : 2;
+    if (((uintptr_t)z | (uintptr_t)out) & (es - 1)) return SD_EINVAL;
+    if (!rules_ok(*rules)) return SD_EINVAL;
+    if (z == out && ld != ld_out) return SD_EINVAL;     // in place: the same rows
+    RulesRows a = {};
+    a.z = z; a.out = out; a.ld = ld; a.ld_out = ld_out; a.rows = rows; a.vocab = vocab;
+    a.r = rule_set(*rules);
+    if (has_penalties(a.r.repetition, a.r.presence, a.r.frequency)) {
+        if (n_tokens < 0 || (n_tokens > 0 && !tokens) || !begin || !end) return SD_EINVAL;
+        if (((uintptr_t)tokens & 3) || (((uintptr_t)begin | (uintptr_t)end) & 7)) return SD_EINVAL;
+        if (n_tokens > 0) { a.tokens = tokens; a.n_tokens = n_tokens; a.begin = begin; a.end = end; }
+    }
+    if (rules->allowed) {
+        if ((uintptr_t)mask_row & 3) return SD_EINVAL;
+        if (!mask_row && rules->n_masks != 1 && rules->n_masks != rows) return SD_EINVAL;
+        a.mask_row = mask_row;
+    }
+    hipStream_t s = (hipStream_t)hip_stream;
+    return (dtype == SD_F32 ? launch<float>(a, s) : launch<bf16_t>(a, s)) == hipSuccess ? SD_OK : SD_EHIP;
+}
