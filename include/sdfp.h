@@ -330,6 +330,31 @@ int sd_logits_rules(const void *z, int dtype, int64_t ld, int32_t rows, int32_t 
                     const int32_t *tokens, int64_t n_tokens, const int64_t *begin, const int64_t *end,
                     const int32_t *mask_row, void *out, int64_t ld_out, void *hip_stream);
 
+/* The two inside a decode context.
+ *
+ * sd_set_draft_head: the draft's forwards end in this output head, MXFP4 panels of [vocab][d_model] as sd_mx4_quantize makes
+ * them from lm_head, instead of lm_head itself: the draft reads 17 / 64 of the bytes of a bfloat16 head.  The draft's
+ * distribution q is then this head's; verification, and with it the distribution of the output (greedy: every token), stays
+ * the target's.  A draft whose skip mask leaves no sub-layer keeps lm_head.  panels: borrowed until sd_free or the next call
+ * of this function; NULL: lm_head again.  Takes effect from the next sd_draft; enqueues nothing.  Errors: SD_EINVAL (ctx,
+ * alignment), SD_ENOMEM (fewer than sd_mx4_bytes(vocab, d_model) bytes).
+ *
+ * sd_set_rules: every row of logits -- the prompt's last, the draft's, the verify rows -- goes through the rules before
+ * anything is picked from it, tested against it or dumped, as if the models' logits were those.  The history of a row is the
+ * prompt, the tokens committed so far (the pending one included) and the draft tokens in front of it.  rules: HOST, copied;
+ * the arrays it names are borrowed.  A grammar: state s allows the tokens of mask s of rules->allowed, and token t leads on
+ * to next[s][t] (DEVICE int32 [n_masks][vocab]; a value outside 0 .. n_masks - 1: no mask from there on); next == NULL: one
+ * mask (n_masks 1) for all rows.  state: where the next pick starts, -1 for no mask; a sequence begun by sd_prefill starts
+ * there again.  A state whose mask allows nothing masks nothing.  (A bias may still leave a row without a number above -inf:
+ * a greedy pick is then token 0, a sampled one the vocabulary's last.)  buf: DEVICE, 256-byte aligned, sd_rules_bytes(cfg,
+ * n_masks) bytes (n_masks 0 without masks), borrowed.  rules == NULL: no rules, the other arguments are ignored.  Called on a
+ * running sequence, the history is what it has so far; sd_set_pending changes neither the history nor the state.  Enqueues on the context's
+ * stream, waits for nothing; the masks have to be final.  Errors: SD_EINVAL (arguments; next without masks, several masks
+ * without next), SD_ENOMEM, SD_ESTATE (between sd_draft and sd_rollback), SD_EHIP. */
+int sd_set_draft_head(sd_ctx *ctx, const void *panels, size_t bytes);
+size_t sd_rules_bytes(const sd_config *cfg, int32_t n_masks);
+int sd_set_rules(sd_ctx *ctx, const sd_rules *rules, const int32_t *next, int32_t state, void *buf, size_t bytes);
+
 #ifdef __cplusplus
 }
 #endif

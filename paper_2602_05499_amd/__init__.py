@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     sd_kv_bytes, sd_workspace_bytes, sd_init, sd_init_static, sd_set_skip_mask, sd_prefill, sd_draft, sd_verify, sd_accept,
     sd_rollback, sd_decode, sd_set_pending, sd_set_draft, sd_read, sd_dump_logits, sd_dump_draft, sd_keep_logits,
     sd_mx4_bytes, sd_mx4_quantize, sd_mx4_dequantize, sd_mx4_matmul, sd_logits_rules, SdRules,
+    sd_set_draft_head, sd_rules_bytes, sd_set_rules,
     sd_phase_trace, sd_phase_trace_read, sd_set_prefill_mode, sd_sync, sd_last_hip_error, sd_free, sd_strerror, EXPORTED_SYMBOLS,
 )
 from .session import Session, build_library  # noqa: F401

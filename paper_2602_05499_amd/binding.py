@@ -23,6 +23,7 @@ EXPORTED_SYMBOLS = (
     "sd_dump_draft", "sd_keep_logits", "sd_phase_trace", "sd_phase_trace_read", "sd_set_spin_limit", "sd_set_turn_span", "sd_set_prefill_mode", "sd_tiled_weights_bytes", "sd_set_tiled_weights", "sd_guard_read", "sd_guard_host_buffer", "sd_sync", "sd_last_hip_error", "sd_free", "sd_strerror",
     "sd_fit_workspace_bytes", "sd_fit_scores", "sd_fit_prune_mask", "sd_fit_prune_sublayers",
     "sd_mx4_bytes", "sd_mx4_quantize", "sd_mx4_dequantize", "sd_mx4_matmul", "sd_logits_rules",
+    "sd_set_draft_head", "sd_rules_bytes", "sd_set_rules",
 )
 
 
@@ -129,6 +130,10 @@ def load_library():
     lib.sd_mx4_dequantize.argtypes = [vp, sz, i32, i32, vp, ci, i64, vp]
     lib.sd_mx4_matmul.argtypes = [vp, sz, i32, i32, vp, ci, i64, i32, vp, ctypes.c_float, vp, ci, i64, vp]
     lib.sd_logits_rules.argtypes = [vp, ci, i64, i32, i32, ctypes.POINTER(SdRules), vp, i64, vp, vp, vp, vp, i64, vp]
+    lib.sd_set_draft_head.argtypes = [vp, vp, sz]
+    lib.sd_rules_bytes.restype = sz
+    lib.sd_rules_bytes.argtypes = [ctypes.POINTER(SdConfig), i32]
+    lib.sd_set_rules.argtypes = [vp, ctypes.POINTER(SdRules), vp, i32, vp, sz]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int and name not in ("sd_kv_bytes", "sd_workspace_bytes", "sd_tiled_weights_bytes"):
@@ -298,6 +303,20 @@ def sd_logits_rules(z_ptr, dtype, ld, rows, vocab, rules, tokens_ptr, n_tokens, 
     """rules: SdRules."""
     return load_library().sd_logits_rules(z_ptr, dtype, ld, rows, vocab, ctypes.byref(rules) if rules is not None else None,
                                           tokens_ptr, n_tokens, begin_ptr, end_ptr, mask_row_ptr, out_ptr, ld_out, stream)
+
+
+def sd_set_draft_head(ctx, panels_ptr, nbytes):
+    """panels_ptr: integer device address (None or 0 detaches the head)."""
+    return load_library().sd_set_draft_head(ctx, panels_ptr or None, int(nbytes))
+
+
+def sd_rules_bytes(cfg, n_masks):
+    return load_library().sd_rules_bytes(ctypes.byref(cfg) if cfg is not None else None, int(n_masks))
+
+
+def sd_set_rules(ctx, rules, next_ptr, state, buf_ptr, nbytes):
+    """rules: SdRules, or None for no rules."""
+    return load_library().sd_set_rules(ctx, ctypes.byref(rules) if rules is not None else None, next_ptr, int(state), buf_ptr, int(nbytes))
 
 
 def sd_set_prefill_mode(ctx, mode):

@@ -2,6 +2,9 @@
 // sequences behind the C-ABI declared in include/sdfp.h (paper Sec. II-A, Alg. 1 Stage B, Sec. III-C).
 #include "sdfp_kernels.hip.h"
 #include "sdfp_prefill.hip.h"
+#include "sdfp_mx4.h"
+#include "sdfp_rules_args.h"
+#include "sdfp_rules_ctx.hip.h"
 #include "sdfp.h"
 
 #include <algorithm>
@@ -234,6 +237,11 @@ struct sd_ctx {
     int prefill_mode;     // -1 = choose (matrix-matrix path for bf16 prompts of PREFILL_MATRIX_MIN_ROWS or more), 0 = 16-row chunks, 1 = matrix-matrix
     PanelPlan panel;      // layout of a prompt panel inside the activation region (matrix-matrix prompt path)
     const char* tiled;    // the layer matrices in the prompt path's tile order (sd_set_tiled_weights), or nullptr
+    const char* draft_head;   // the draft's output head in MXFP4 panels (sd_set_draft_head), or nullptr
+    const float* draft_row;   // where a draft forward without output head leaves its row; nullptr if no sub-layer runs
+    CtxRules rules;           // rules on logits (sd_set_rules); counts == nullptr: none
+    int rules_start;          // the grammar's state in front of the prompt's first pick
+    int n_prompt;             // length of the prompt in the workspace
     const char *w_lo, *w_hi;   // address range spanned by the weight tensors (guard build)
     unsigned long long* dbg_host;   // pinned host buffer for guard records and beacons (guard build), or nullptr
 
@@ -339,7 +347,7 @@ void link_projections(std::vector<Phase>& prog) {   // Phase::link, from the end
 // The phase list of one forward: embedding, then for every layer the sub-layers that are not skipped, then
 // the output head.  A skipped sub-layer contributes nothing and writes no keys / values (Alg. 1: the draft is
 // the target minus the prune set); the residual stream simply passes to the next phase that runs.
-std::vector<Phase> build_program(const sd_ctx* c, bool use_skip) {
+std::vector<Phase> build_program(const sd_ctx* c, bool use_skip, const float** last_row = nullptr) {
     const sd_config& g = c->cfg;
     const Carve& cv = c->cv;
     const size_t esz = esize(&g);
@@ -406,6 +414,7 @@ std::vector<Phase> build_program(const sd_ctx* c, bool use_skip) {
             h = h2;
         }
     }
+    if (last_row) *last_row = prog.size() > 1 ? h : nullptr;
     {
         Phase p = blank(PK_HEAD, -1);
         p.Kd = g.d_model; p.N = g.vocab; p.n_units = p.N;
@@ -418,7 +427,9 @@ std::vector<Phase> build_program(const sd_ctx* c, bool use_skip) {
 }
 
 int upload_program(sd_ctx* c, bool draft) {
-    std::vector<Phase> prog = build_program(c, draft);
+    const float* last_row = nullptr;
+    std::vector<Phase> prog = build_program(c, draft, &last_row);
+    if (draft) c->draft_row = last_row;
     c->n_prog[draft ? 1 : 0] = (int)prog.size();
     HIPCHK(c, hipMemcpyAsync(c->ws + (draft ? c->cv.prog_draft : c->cv.prog_target), prog.data(),
                              prog.size() * sizeof(Phase), hipMemcpyHostToDevice, c->stream));
@@ -795,6 +806,24 @@ void pick_sample(sd_ctx* c, const float* z, float u, int dst, int off) {
                        c->sel(), c->st(), dst, off);
 }
 
+// rules on rows of logits, in place, and (greedy) their arg-maxes into st->d[off ..] / st->amax[off ..]; row 0 comes after r0
+// draft tokens
+void select_rows(sd_ctx* c, float* z, int rows, int r0, int mode, int dst, int off) {
+    const int V = c->cfg.vocab, len = rules_chunk_len(V);
+    hipLaunchKernelGGL(k_rows_select, dim3((V + len - 1) / len, rows), dim3(RULES_THREADS), 0, c->stream, z, V, len, c->rules, r0,
+                       mode == SD_GREEDY ? 1 : 0, c->sel(), c->st(), dst, off);
+}
+// the history's counts and the grammar's state: of the prompt alone, or of the running sequence
+void rules_begin(sd_ctx* c, bool running) {
+    const int V = c->cfg.vocab;
+    hipLaunchKernelGGL(k_zero_u32, dim3(64), dim3(256), 0, c->stream, c->rules.counts, V);
+    hipLaunchKernelGGL(k_rules_history, dim3(16), dim3(256), 0, c->stream, c->rules, V, c->rules_start, c->prompt(), c->n_prompt,
+                       running ? c->out_tokens() : (const int*)nullptr, c->st());
+}
+void rules_commit(sd_ctx* c) {
+    hipLaunchKernelGGL(k_rules_commit, dim3(1), dim3(64), 0, c->stream, c->rules, c->cfg.vocab, c->st());
+}
+
 template <typename WT>
 int do_prefill(sd_ctx* c, const int32_t* prompt_host, int n, int mode, const float* u_host) {
     int e = lazy_device_init(c);
@@ -803,7 +832,9 @@ int do_prefill(sd_ctx* c, const int32_t* prompt_host, int n, int mode, const flo
     HIPCHK(c, hipStreamSynchronize(c->stream));   // prompt_host may be reused by the caller on return
     // a fresh sequence starts from clean barrier counters (also the way out of SD_ETIMEOUT)
     hipLaunchKernelGGL(k_zero_u32, dim3(1), dim3(64), 0, c->stream, reinterpret_cast<unsigned*>(c->ws + c->cv.bar), BAR_WORDS + 1);
-    const bool keep = mode == SD_SAMPLE || c->keep_logits;
+    const bool ruled = c->rules.counts != nullptr;
+    const bool keep = mode == SD_SAMPLE || c->keep_logits || ruled;
+    c->n_prompt = n;
     const bool gemm = std::is_same<WT, bf16_t>::value && c->panel.P > 0 && pf_panels_hold(c->cfg.head_dim, n) &&
                       (c->prefill_mode == 1 || (c->prefill_mode < 0 && n >= PREFILL_MATRIX_MIN_ROWS));
     if (gemm) {
@@ -818,8 +849,13 @@ int do_prefill(sd_ctx* c, const int32_t* prompt_host, int n, int mode, const flo
             if ((e = forward<WT>(c, rows, PROG_TARGET, hp))) return e;
         }
     }
+    if (ruled) {
+        rules_begin(c, false);
+        select_rows(c, c->f(c->cv.zp), 1, 0, mode, (int)ROWS_VERIFY, 0);
+    }
     if (mode == SD_SAMPLE) pick_sample(c, c->f(c->cv.zp), u_host[0], (int)ROWS_VERIFY, 0);
     hipLaunchKernelGGL(k_commit_first, dim3(1), dim3(64), 0, c->stream, c->st(), c->out_tokens(), n);
+    if (ruled) rules_commit(c);
     HIPCHK(c, hipGetLastError());
     return SD_OK;
 }
@@ -829,11 +865,20 @@ int do_draft(sd_ctx* c, int K, int mode, const float* u_host) {
     hipLaunchKernelGGL(k_set_k, dim3(1), dim3(64), 0, c->stream, c->st(), K);
     for (int i = 0; i < K; ++i) {
         Rows rows{1, ROWS_DRAFT, i};
-        const bool keep = (mode == SD_SAMPLE) || c->keep_logits;
-        HeadPlan hp{true, 0, keep ? c->f(c->cv.zq) + (size_t)i * c->cfg.vocab : nullptr, ROWS_DRAFT, i};
+        float* z = c->f(c->cv.zq) + (size_t)i * c->cfg.vocab;
+        const bool ruled = c->rules.counts != nullptr, mx4 = c->draft_head && c->draft_row;
+        const bool keep = (mode == SD_SAMPLE) || c->keep_logits || ruled;
+        HeadPlan hp{!mx4, 0, keep && !mx4 ? z : nullptr, ROWS_DRAFT, i};
         int e = forward<WT>(c, rows, PROG_DRAFT, hp);
         if (e) return e;
-        if (mode == SD_SAMPLE) pick_sample(c, c->f(c->cv.zq) + (size_t)i * c->cfg.vocab, u_host[i], (int)ROWS_DRAFT, i);
+        if (mx4) {
+            const sd_config& g = c->cfg;
+            const Mx4Product p{c->draft_head, c->draft_row, c->final_norm, z, g.d_model, g.vocab, 1, g.vocab, g.d_model, MX4_X_F32, MX4_X_F32,
+                               g.rms_eps};
+            HIPCHK(c, mx4_product(p, c->stream));
+        }
+        if (ruled || (mx4 && mode == SD_GREEDY)) select_rows(c, z, 1, i, mode, (int)ROWS_DRAFT, i);
+        if (mode == SD_SAMPLE) pick_sample(c, z, u_host[i], (int)ROWS_DRAFT, i);
     }
     HIPCHK(c, hipGetLastError());
     return SD_OK;
@@ -842,9 +887,14 @@ int do_draft(sd_ctx* c, int K, int mode, const float* u_host) {
 template <typename WT>
 int do_verify(sd_ctx* c) {
     Rows rows{c->K_cur + 1, ROWS_VERIFY, 0};
-    const bool keep = (c->mode_cur == SD_SAMPLE) || c->keep_logits;
+    const bool ruled = c->rules.counts != nullptr;
+    const bool keep = (c->mode_cur == SD_SAMPLE) || c->keep_logits || ruled;
     HeadPlan hp{true, 0, keep ? c->f(c->cv.zp) : nullptr, ROWS_VERIFY, 0};
-    return forward<WT>(c, rows, PROG_TARGET, hp);
+    int e = forward<WT>(c, rows, PROG_TARGET, hp);
+    if (e || !ruled) return e;
+    select_rows(c, c->f(c->cv.zp), rows.M, 0, c->mode_cur, (int)ROWS_VERIFY, 0);
+    HIPCHK(c, hipGetLastError());
+    return SD_OK;
 }
 
 int do_accept(sd_ctx* c, int mode, const float* u_host) {
@@ -860,6 +910,7 @@ int do_accept(sd_ctx* c, int mode, const float* u_host) {
         hipLaunchKernelGGL(k_accept_sample, dim3(chunks), dim3(SEL_THREADS), 0, c->stream, c->f(c->cv.zq), c->f(c->cv.zp), V, len,
                            c->cfg.temperature, c->K_cur, un, c->sel(), c->st(), c->out_tokens());
     }
+    if (c->rules.counts) rules_commit(c);
     HIPCHK(c, hipGetLastError());
     return SD_OK;
 }
@@ -927,6 +978,9 @@ void fill_ctx(sd_ctx* c, LayerPtrs* layers, uint8_t* skip, const sd_config* cfg,
     c->static_dev = -1;
     c->prefill_mode = -1;
     c->tiled = nullptr;
+    c->draft_head = nullptr; c->draft_row = nullptr;
+    c->rules = CtxRules{};
+    c->rules_start = 0; c->n_prompt = 0;
     c->panel = plan_panel(cfg, c->cv.acts_bytes);
     const size_t es = esize(cfg), d = (size_t)cfg->d_model, hq = (size_t)cfg->n_heads * cfg->head_dim,
                  hkv = (size_t)cfg->n_kv_heads * cfg->head_dim, F = (size_t)cfg->d_ffn, V = (size_t)cfg->vocab;
@@ -1234,6 +1288,46 @@ int sd_set_tiled_weights(sd_ctx* c, void* buf, size_t bytes) {
     if (e != hipSuccess) { c->hip_err = (int)e; return SD_EHIP; }
     c->tiled = (const char*)buf;
     return reupload();
+}
+
+int sd_set_draft_head(sd_ctx* c, const void* panels, size_t bytes) {
+    if (!c) return SD_EINVAL;
+    if (!panels) { c->draft_head = nullptr; return SD_OK; }
+    if ((uintptr_t)panels & 255) return SD_EINVAL;
+    if (bytes < mx4_bytes(c->cfg.vocab, c->cfg.d_model)) return SD_ENOMEM;
+    c->draft_head = (const char*)panels;
+    return SD_OK;
+}
+
+size_t sd_rules_bytes(const sd_config* cfg, int32_t n_masks) {
+    if (!config_ok(cfg) || n_masks < 0) return 0;
+    return align_up((size_t)cfg->vocab * 4) + align_up(4) + align_up((size_t)n_masks * 4);
+}
+
+int sd_set_rules(sd_ctx* c, const sd_rules* rules, const int32_t* next, int32_t state, void* buf, size_t bytes) {
+    if (!c) return SD_EINVAL;
+    if (rules) {
+        if (!rules_ok(*rules) || !buf || ((uintptr_t)buf & 255) || ((uintptr_t)next & 3)) return SD_EINVAL;
+        if (rules->allowed ? state < -1 || state >= rules->n_masks : next != nullptr) return SD_EINVAL;
+        if (!next && rules->allowed && rules->n_masks != 1) return SD_EINVAL;
+        if (bytes < sd_rules_bytes(&c->cfg, rules->allowed ? rules->n_masks : 0)) return SD_ENOMEM;
+    }
+    if (c->phase != PH_INIT && c->phase != PH_READY) return SD_ESTATE;   // a step is judged by the rules it was drafted under
+    if (!rules) { c->rules = CtxRules{}; return SD_OK; }
+    CtxRules r = {};
+    r.r = rule_set(*rules);
+    r.next = next;
+    char* at = (char*)buf;
+    r.counts = (unsigned*)at; at += align_up((size_t)c->cfg.vocab * 4);
+    r.state = (int*)at; at += align_up(4);
+    int* usable = (int*)at;
+    r.usable = usable;
+    c->rules = r;
+    c->rules_start = rules->allowed ? state : -1;
+    if (r.r.allowed) hipLaunchKernelGGL(k_rules_usable, dim3((unsigned)r.r.n_masks), dim3(256), 0, c->stream, r.r.allowed, c->cfg.vocab, usable);
+    if (c->phase == PH_READY) rules_begin(c, true);
+    HIPCHK(c, hipGetLastError());
+    return SD_OK;
 }
 
 int sd_set_prefill_mode(sd_ctx* c, int mode) {

@@ -143,6 +143,10 @@ class Session:
             self.ctx = None
         self._check(rc, "sd_init_static" if static_workspace else "sd_init")
         self.max_seq, self.max_k, self.max_out = max_seq, max_k, max_out
+        # what the context borrows from set_draft_head and set_rules, and what it may still be reading from earlier calls of
+        # them (let go when the stream has been waited for)
+        self.draft_head = self.rules = None
+        self._retired = []
         # bfloat16 storage: a second copy of the layer matrices in the tile order of the matrix-matrix prompt path
         # (sd_set_tiled_weights; optional, the prompt path reads the caller's matrices without it, more slowly)
         # tiled_weights: True = attach it (an allocation failure is raised), False = never, None = attach it if the
@@ -234,6 +238,54 @@ class Session:
         self.tiled = self.torch.empty(need, dtype=self.torch.uint8, device=self.kv.device)
         self._check(B.sd_set_tiled_weights(self.ctx, self.tiled.data_ptr(), need), "sd_set_tiled_weights")
 
+    def set_draft_head(self, head=True):
+        """The draft's output head in MXFP4 (sd_set_draft_head): an Mx4 of [vocab][d_model], True to quantise the model's
+        lm_head, False or None to go back to lm_head."""
+        if head is None or head is False:
+            self._check(B.sd_set_draft_head(self.ctx, None, 0), "sd_set_draft_head")
+            self.sync()
+            self.draft_head = None
+            return
+        from .operators import Mx4, mx4_quantize
+        if head is True:
+            with self.torch.cuda.stream(self.stream):
+                head = mx4_quantize(self.weights.lm_head)
+        s = self.shape
+        if not isinstance(head, Mx4) or (head.rows, head.cols) != (s.vocab, s.d_model) or head.data.device != self.kv.device:
+            raise B.SdError(B.SD_EINVAL, "set_draft_head")
+        self._check(B.sd_set_draft_head(self.ctx, head.data.data_ptr(), head.data.numel()), "sd_set_draft_head")
+        self._retired.append(self.draft_head)
+        self.draft_head = head
+
+    def set_rules(self, *, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, next=None, state=0):
+        """Rules on every row of logits before a token is picked from it (sd_set_rules).  bias: float32 [vocab]; allowed:
+        int32 or uint32 [n_masks][ceil(vocab / 32)]; next: int32 [n_masks][vocab], the grammar's state behind each token;
+        state: the start.  Called without arguments: no rules."""
+        torch, s, dev = self.torch, self.shape, self.kv.device
+        if repetition == 1.0 and presence == 0.0 and frequency == 0.0 and bias is None and allowed is None and next is None:
+            self._check(B.sd_set_rules(self.ctx, None, None, 0, None, 0), "sd_set_rules")
+            self.sync()
+            self.rules = None
+            return
+
+        def ptr(t, types, dims):
+            if t is None:
+                return None
+            if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype not in types or tuple(t.shape) != dims or not t.is_contiguous():
+                raise B.SdError(B.SD_EINVAL, "set_rules")
+            return t.data_ptr()
+
+        n = 0 if allowed is None else allowed.shape[0]
+        r = B.SdRules(repetition, presence, frequency, ptr(bias, (torch.float32,), (s.vocab,)),
+                      ptr(allowed, (torch.int32, torch.uint32), (n, (s.vocab + 31) // 32)), n)
+        nx = ptr(next, (torch.int32,), (n, s.vocab))
+        need = B.sd_rules_bytes(self.cfg, n)
+        with torch.cuda.stream(self.stream):
+            buf = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._check(B.sd_set_rules(self.ctx, r, nx, state, buf.data_ptr(), need), "sd_set_rules")
+        self._retired.append(self.rules)
+        self.rules = (buf, bias, allowed, next)
+
     def phase_trace(self, on=True):
         self._check(B.sd_phase_trace(self.ctx, on), "sd_phase_trace")
 
@@ -259,6 +311,7 @@ class Session:
 
     def sync(self):
         self._check(B.sd_sync(self.ctx), "sd_sync")
+        self._retired.clear()
 
     def read(self, cap: Optional[int] = None):
         """Returns (tokens int32[n], stats dict).  Waits for the stream."""

@@ -103,3 +103,46 @@ def test_the_rules_struct_has_the_headers_layout():
     assert [n for n, _ in B.SdRules._fields_][:3] == ["repetition", "presence", "frequency"]
     assert B.SdRules.bias.offset == 16 and B.SdRules.allowed.offset == 24 and B.SdRules.n_masks.offset == 32
     assert ctypes.sizeof(B.SdRules) == 40
+
+
+def _context(**over):
+    L = 2
+    base = dict(n_layers=L, d_model=64, n_heads=2, n_kv_heads=2, head_dim=32, d_ffn=64, vocab=100, max_seq=64, max_k=4, dtype=B.SD_F32,
+                max_out=64, rms_eps=1e-5, rope_theta=10000.0, temperature=1.0)
+    base.update(over)
+    cfg = B.SdConfig(*[base[n] for n, _ in B.SdConfig._fields_])
+    arrs = [(ctypes.c_void_p * L)(*[A + 4096 * (i + 1) for i in range(L)]) for _ in range(9)]
+    w = B.SdWeights(A, A + 256, A + 512, *[ctypes.cast(a, ctypes.POINTER(ctypes.c_void_p)) for a in arrs])
+    rc, ctx = B.sd_init(cfg, w, None, A, B.sd_kv_bytes(cfg), A, B.sd_workspace_bytes(cfg), None)
+    assert rc == B.SD_OK
+    return cfg, ctx, arrs
+
+
+def test_draft_head_is_checked_on_the_host():
+    cfg, ctx, keep = _context()
+    n = B.sd_mx4_bytes(cfg.vocab, cfg.d_model)
+    assert B.sd_set_draft_head(ctx, A, n) == B.SD_OK and B.sd_set_draft_head(ctx, None, 0) == B.SD_OK
+    assert B.sd_set_draft_head(ctx, A + 16, n) == B.SD_EINVAL
+    assert B.sd_set_draft_head(ctx, A, n - 1) == B.SD_ENOMEM
+    assert B.sd_set_draft_head(ctypes.c_void_p(None), A, n) == B.SD_EINVAL
+    B.sd_free(ctx)
+
+
+def test_context_rules_are_checked_on_the_host():
+    cfg, ctx, keep = _context()
+    assert B.sd_rules_bytes(cfg, -1) == 0 and B.sd_rules_bytes(None, 0) == 0
+    n0, n1, n70 = (B.sd_rules_bytes(cfg, n) for n in (0, 1, 70))
+    assert n0 == 512 + 256 and n1 == n0 + 256 and n70 == n0 + 512
+    ok = _rules(presence=1.0)
+    for call in (lambda: (ok, None, 0, None, n0), lambda: (ok, None, 0, A + 8, n0), lambda: (_rules(repetition=-1.0), None, 0, A, n0),
+                 lambda: (ok, A, 0, A, n0),                                                   # next without masks
+                 lambda: (_rules(allowed=A, n_masks=2), None, 0, A, n70),                     # several masks without next
+                 lambda: (_rules(allowed=A, n_masks=2), A + 2, 0, A, n70),
+                 lambda: (_rules(allowed=A, n_masks=2), A, 2, A, n70), lambda: (_rules(allowed=A, n_masks=2), A, -2, A, n70),
+                 lambda: (_rules(allowed=A, n_masks=0), A, -1, A, n70), lambda: (_rules(bias=A + 1), None, 0, A, n0)):
+        assert B.sd_set_rules(ctx, *call()) == B.SD_EINVAL
+    assert B.sd_set_rules(ctx, ok, None, 0, A, n0 - 1) == B.SD_ENOMEM
+    assert B.sd_set_rules(ctx, _rules(allowed=A, n_masks=70), A, 0, A, n70 - 1) == B.SD_ENOMEM
+    assert B.sd_set_rules(ctx, None, None, 0, None, 0) == B.SD_OK
+    assert B.sd_set_rules(ctypes.c_void_p(None), ok, None, 0, A, n0) == B.SD_EINVAL
+    B.sd_free(ctx)
