@@ -8,41 +8,51 @@ import torch
 
 from . import binding as B
 
+# A call's time on the host is its cost wherever the kernel takes a few microseconds, so the checks below use the cheapest form
+# of each question: device indexes instead of device objects, the raw handle of the current stream (torch.cuda.current_stream
+# builds an object: 2.0 us against 0.1).
 _CODES = {torch.float32: B.SD_F32, torch.bfloat16: B.SD_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _require(ok, what):
-    if not ok:
-        raise B.SdError(B.SD_EINVAL, what)
+def _refuse(what):
+    raise B.SdError(B.SD_EINVAL, what)
 
 
-def _check(rc, where):
+def _on(index, fn, *args):
+    """fn(*args, current stream of device `index`), with the device current; a code other than SD_OK is raised."""
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
     if rc != B.SD_OK:
-        raise B.SdError(rc, where)
+        raise B.SdError(rc, fn.__name__)
 
 
-def _on(device, fn, *args):
-    """fn(*args, current stream of device), with the device current."""
-    if torch.cuda.current_device() == device.index:
-        return fn(*args, torch.cuda.current_stream(device).cuda_stream)
-    with torch.cuda.device(device):
-        return fn(*args, torch.cuda.current_stream(device).cuda_stream)
-
-
-def _rows(t, where, types=_CODES):
-    """(rows, columns, distance of rows) of a 2-D tensor whose rows are contiguous."""
-    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in types, where)
+def _rows(t, where):
+    """(rows, columns, distance of rows, type code) of a 2-D tensor on a GPU whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        _refuse(where)
     n, c = t.shape
-    _require(n > 0 and c > 0 and (c == 1 or t.stride(1) == 1), where)
-    ld = t.stride(0) if n > 1 else c
-    _require(ld >= c, where)
-    return n, c, ld
+    ld, step = t.stride()
+    code = _CODES.get(t.dtype)
+    if n == 1:
+        ld = c
+    if code is None or n < 1 or c < 1 or (step != 1 and c != 1) or ld < c:
+        _refuse(where)
+    return n, c, ld, code
 
 
-def _vector(t, dtype, n, device, where):
-    _require(isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and t.dim() == 1 and t.is_contiguous() and
-             (n is None or t.numel() == n), where)
+def _array(t, dtypes, shape, index, where):
+    """The address of a contiguous tensor of one of `dtypes` and of `shape` (None: any vector) on device `index`."""
+    if (not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.get_device() != index or not t.is_contiguous() or
+            (t.shape != shape if shape is not None else t.dim() != 1)):
+        _refuse(where)
     return t.data_ptr()
+
+
+_I32, _I64, _F32, _BITS = (torch.int32,), (torch.int64,), (torch.float32,), (torch.int32, torch.uint32)
 
 
 class Mx4:
@@ -52,8 +62,9 @@ class Mx4:
 
     def __init__(self, data, rows, cols):
         need = B.sd_mx4_bytes(rows, cols)
-        _require(isinstance(data, torch.Tensor) and data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous() and
-                 need > 0 and data.numel() >= need and data.data_ptr() % 256 == 0, "Mx4: a contiguous, aligned uint8 tensor of the matrix's size")
+        if (not isinstance(data, torch.Tensor) or not data.is_cuda or data.dtype != torch.uint8 or not data.is_contiguous() or need == 0 or
+                data.numel() < need or data.data_ptr() % 256):
+            _refuse("Mx4: a contiguous, 256-byte aligned uint8 tensor of at least the matrix's size on a GPU")
         self.data, self.rows, self.cols = data, rows, cols
 
     def __repr__(self):
@@ -62,45 +73,49 @@ class Mx4:
 
 def mx4_quantize(x) -> Mx4:
     """Rows of float32 or bfloat16 in MXFP4 (sd_mx4_quantize)."""
-    rows, cols, ld = _rows(x, "mx4_quantize: x")
+    rows, cols, ld, code = _rows(x, "mx4_quantize: x")
     n = B.sd_mx4_bytes(rows, cols)
-    q = torch.empty(n, dtype=torch.uint8, device=x.device)
-    _check(_on(x.device, B.sd_mx4_quantize, x.data_ptr(), _CODES[x.dtype], ld, rows, cols, q.data_ptr(), n), "sd_mx4_quantize")
-    return Mx4(q, rows, cols)
+    data = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _on(x.get_device(), B.sd_mx4_quantize, x.data_ptr(), code, ld, rows, cols, data.data_ptr(), n)
+    q = Mx4.__new__(Mx4)
+    q.data, q.rows, q.cols = data, rows, cols
+    return q
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.float32):
     """The values of an MXFP4 matrix as rows of float32 or bfloat16, both exact (sd_mx4_dequantize)."""
-    _require(isinstance(q, Mx4) and dtype in _CODES, "mx4_dequantize: q, dtype")
-    x = torch.empty(q.rows, q.cols, dtype=dtype, device=q.data.device)
-    _check(_on(x.device, B.sd_mx4_dequantize, q.data.data_ptr(), q.data.numel(), q.rows, q.cols, x.data_ptr(), _CODES[dtype], q.cols),
-           "sd_mx4_dequantize")
+    code = _CODES.get(dtype)
+    if not isinstance(q, Mx4) or code is None:
+        _refuse("mx4_dequantize: q, dtype")
+    d, cols = q.data, q.cols
+    x = torch.empty((q.rows, cols), dtype=dtype, device=d.device)
+    _on(d.get_device(), B.sd_mx4_dequantize, d.data_ptr(), d.numel(), q.rows, cols, x.data_ptr(), code, cols)
     return x
 
 
 def mx4_matmul(x, w: Mx4, gain=None, eps: float = 1e-5, out_dtype=None):
     """x w^T (sd_mx4_matmul).  x: rows of float32 or bfloat16, or an Mx4; gain (float32 x only): RMS-normalise the rows and
     multiply by it first.  The result has x's type, float32 for an Mx4, or out_dtype (float32 or bfloat16)."""
-    _require(isinstance(w, Mx4), "mx4_matmul: w")
-    dev = w.data.device
+    if not isinstance(w, Mx4):
+        _refuse("mx4_matmul: w")
+    wd, n = w.data, w.rows
+    index = wd.get_device()
     if isinstance(x, Mx4):
-        m, k, ldx, code, ptr, dt = x.rows, x.cols, x.data.numel(), B.SD_MX4, x.data.data_ptr(), torch.float32
-        _require(x.data.device == dev, "mx4_matmul: x and w on one device")
+        m, k, xd, code, dtype = x.rows, x.cols, x.data, B.SD_MX4, torch.float32
+        ld = xd.numel()
     else:
-        m, k, ldx = _rows(x, "mx4_matmul: x")
-        code, ptr, dt = _CODES[x.dtype], x.data_ptr(), x.dtype
-        _require(x.device == dev, "mx4_matmul: x and w on one device")
-    _require(k == w.cols, "mx4_matmul: columns of x and w")
+        m, k, ld, code = _rows(x, "mx4_matmul: x")
+        xd, dtype = x, x.dtype
+    if k != w.cols or xd.get_device() != index:
+        _refuse("mx4_matmul: x and w of one width on one device")
     if out_dtype is not None:
-        _require(out_dtype in _CODES, "mx4_matmul: out_dtype")
-        dt = out_dtype
-    g = None
-    if gain is not None:
-        _require(code == B.SD_F32, "mx4_matmul: a gain goes with float32 x")
-        g = _vector(gain, torch.float32, k, dev, "mx4_matmul: gain")
-    y = torch.empty(m, w.rows, dtype=dt, device=dev)
-    _check(_on(dev, B.sd_mx4_matmul, w.data.data_ptr(), w.data.numel(), w.rows, k, ptr, code, ldx, m, g, eps, y.data_ptr(),
-               _CODES[dt], w.rows), "sd_mx4_matmul")
+        dtype = out_dtype
+    y_code = _CODES.get(dtype)
+    if y_code is None or (gain is not None and code != B.SD_F32):
+        _refuse("mx4_matmul: out_dtype, or a gain without float32 x")
+    g = None if gain is None else _array(gain, _F32, (k,), index, "mx4_matmul: gain")
+    y = torch.empty((m, n), dtype=dtype, device=wd.device)
+    _on(index, B.sd_mx4_matmul, wd.data_ptr(), wd.numel(), n, k, xd.data_ptr(), code, ld, m, g, eps, y.data_ptr(), y_code, n)
     return y
 
 
@@ -112,30 +127,27 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
     bias: float32 [vocab].  allowed: int32 or uint32 [n_masks][ceil(vocab / 32)], bit j % 32 of word j // 32 allows token j;
     mask_row: int32 [rows], the mask of each row (-1: none); by default row i has mask i, or all have the only one.
     out: where the result goes (`logits` itself: in place); by default a new tensor."""
-    rows, vocab, ld = _rows(logits, "logits_rules: logits")
-    dev = logits.device
+    rows, vocab, ld, code = _rows(logits, "logits_rules: logits")
+    index = logits.get_device()
     if out is None:
-        out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
-        ld_out = vocab
+        out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
     else:
-        r, v, ld_out = _rows(out, "logits_rules: out", (logits.dtype,))
-        _require((r, v) == (rows, vocab) and out.device == dev, "logits_rules: out")
-    t = b = e = m = None
-    n = 0
+        r, v, ld_out, c = _rows(out, "logits_rules: out")
+        if r != rows or v != vocab or c != code or out.get_device() != index:
+            _refuse("logits_rules: out")
+    t = b = e = p_bias = p_allowed = m = None
+    n = n_masks = 0
     if repetition != 1.0 or presence != 0.0 or frequency != 0.0:
-        t, n = _vector(tokens, torch.int32, None, dev, "logits_rules: tokens"), tokens.numel()
-        b = _vector(begin, torch.int64, rows, dev, "logits_rules: begin")
-        e = _vector(end, torch.int64, rows, dev, "logits_rules: end")
-    rules = B.SdRules(repetition, presence, frequency, None, None, 0)
+        t, n = _array(tokens, _I32, None, index, "logits_rules: tokens"), tokens.numel()
+        b = _array(begin, _I64, (rows,), index, "logits_rules: begin")
+        e = _array(end, _I64, (rows,), index, "logits_rules: end")
     if bias is not None:
-        rules.bias = _vector(bias, torch.float32, vocab, dev, "logits_rules: bias")
+        p_bias = _array(bias, _F32, (vocab,), index, "logits_rules: bias")
     if allowed is not None:
-        _require(isinstance(allowed, torch.Tensor) and allowed.device == dev and allowed.dtype in (torch.int32, torch.uint32) and
-                 allowed.dim() == 2 and allowed.is_contiguous() and allowed.shape[0] > 0 and allowed.shape[1] == (vocab + 31) // 32,
-                 "logits_rules: allowed")
-        rules.allowed, rules.n_masks = allowed.data_ptr(), allowed.shape[0]
+        n_masks = allowed.shape[0] if isinstance(allowed, torch.Tensor) and allowed.dim() else 0
+        p_allowed = _array(allowed, _BITS, (n_masks, (vocab + 31) // 32), index, "logits_rules: allowed")
         if mask_row is not None:
-            m = _vector(mask_row, torch.int32, rows, dev, "logits_rules: mask_row")
-    _check(_on(dev, B.sd_logits_rules, logits.data_ptr(), _CODES[logits.dtype], ld, rows, vocab, rules, t, n, b, e, m, out.data_ptr(),
-               ld_out), "sd_logits_rules")
+            m = _array(mask_row, _I32, (rows,), index, "logits_rules: mask_row")
+    _on(index, B.sd_logits_rules, logits.data_ptr(), code, ld, rows, vocab,
+        B.SdRules(repetition, presence, frequency, p_bias, p_allowed, n_masks), t, n, b, e, m, out.data_ptr(), ld_out)
     return out
