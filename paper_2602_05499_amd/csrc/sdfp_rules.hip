@@ -6,14 +6,16 @@ using namespace sdfp;
 
 namespace {
 
-// The shortest chunk, unless a longer one still gives every compute unit two workgroups.
+// Short chunks for few rows: 2048 entries of a 512-thread workgroup, one quad of them per thread (one row of 32000 3.3 us, 4096
+// entries 4.0 to 6.0; five of 128256 4.6 against 5.2 to 6.8).  Once 4096-entry chunks of 256 threads still make four
+// workgroups per compute unit, those: a row's history is read half as often (256 rows of 32003 in bfloat16 13.4 us against
+// 16.7, 64 of 128256 13.8 against 16.4 -- 4.9 TB/s, a large copy 4.7).
 template <typename T>
 hipError_t launch(const RulesRows& a, hipStream_t s) {
     auto chunks = [&](int ch) { return (int64_t)a.rows * ((a.vocab + ch - 1) / ch); };
-    if (chunks(1024) > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (chunks(8192) >= 512) hipLaunchKernelGGL((k_logits_rules<T, 8192>), dim3((unsigned)chunks(8192)), dim3(RULES_THREADS), 0, s, a);
-    else if (chunks(4096) >= 512) hipLaunchKernelGGL((k_logits_rules<T, 4096>), dim3((unsigned)chunks(4096)), dim3(RULES_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((k_logits_rules<T, 1024>), dim3((unsigned)chunks(1024)), dim3(RULES_THREADS), 0, s, a);
+    if (chunks(2048) > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (chunks(4096) >= 1024) hipLaunchKernelGGL((k_logits_rules<T, 256, 4>), dim3((unsigned)chunks(4096)), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_logits_rules<T, 512, 1>), dim3((unsigned)chunks(2048)), dim3(512), 0, s, a);
     return hipGetLastError();
 }
 

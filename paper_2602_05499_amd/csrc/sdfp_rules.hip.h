@@ -72,30 +72,39 @@ struct RulesRows {
     const int64_t *begin, *end;   // [rows]: the row's history is tokens[begin .. end)
     const int* mask_row;          // [rows] or nullptr: row i under mask i (mask 0 if there is one mask)
 };
-template <typename T, int CH>
-__global__ __launch_bounds__(RULES_THREADS) void k_logits_rules(RulesRows a) {
-    constexpr int NV = CH / (RULES_THREADS * 4);
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void k_logits_rules(RulesRows a) {
+    constexpr int CH = THREADS * 4 * NV;
     __shared__ __attribute__((aligned(16))) unsigned cnt[CH];
     const int tid = threadIdx.x, chunks = (a.vocab + CH - 1) / CH, row = blockIdx.x / chunks;
     const int lo = (blockIdx.x - row * chunks) * CH;
     const T* z = reinterpret_cast<const T*>(a.z) + (int64_t)row * a.ld + lo;
     const int have = a.vocab - lo;
-    f32x4 v[NV];
+    const unsigned* mask = nullptr;
+    if (a.r.allowed) {
+        const int mr = a.mask_row ? a.mask_row[row] : a.r.n_masks == 1 ? 0 : row;
+        if (mr >= 0 && mr < a.r.n_masks) mask = a.r.allowed + (int64_t)mr * ((a.vocab + 31) / 32) + (lo >> 5);
+    }
+    // everything that the entries need is on its way while the history is counted
+    f32x4 v[NV], bi[NV];
+    unsigned w[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int j = (i * RULES_THREADS + tid) * 4;
+        const int j = (i * THREADS + tid) * 4;
         v[i] = rules_load4(z + j, have - j);
+        if (a.r.bias) bi[i] = rules_load4(a.r.bias + lo + j, have - j);
+        if (mask && j < have) w[i] = mask[j >> 5];
     }
     if (a.tokens) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(cnt + (i * RULES_THREADS + tid) * 4) = u32x4{0u, 0u, 0u, 0u};
+        for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(cnt + (i * THREADS + tid) * 4) = u32x4{0u, 0u, 0u, 0u};
         const int64_t b = max(a.begin[row], (int64_t)0), e = min(a.end[row], a.n_tokens);
         __syncthreads();
         auto count = [&](int tok) {
             const unsigned at = (unsigned)tok - (unsigned)lo;
             if (at < (unsigned)CH && tok >= 0) atomicAdd(&cnt[at], 1u);
         };
-        for (int64_t i = b + tid * 4; i < e; i += RULES_THREADS * 4) {
+        for (int64_t i = b + tid * 4; i < e; i += THREADS * 4) {
             if (i + 4 <= e) {
                 const u32x4 t = *reinterpret_cast<const SDFP_GLOBAL u32x4_w*>(as_global(a.tokens + i));
                 count((int)t.x); count((int)t.y); count((int)t.z); count((int)t.w);
@@ -105,32 +114,24 @@ __global__ __launch_bounds__(RULES_THREADS) void k_logits_rules(RulesRows a) {
         }
         __syncthreads();
     }
-    const unsigned* mask = nullptr;
-    if (a.r.allowed) {
-        const int mr = a.mask_row ? a.mask_row[row] : a.r.n_masks == 1 ? 0 : row;
-        if (mr >= 0 && mr < a.r.n_masks) mask = a.r.allowed + (int64_t)mr * ((a.vocab + 31) / 32);
-    }
     T* out = reinterpret_cast<T*>(a.out) + (int64_t)row * a.ld_out + lo;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int j = (i * RULES_THREADS + tid) * 4;
+        const int j = (i * THREADS + tid) * 4;
         if (j >= have) continue;
         f32x4 x = v[i];
         if (a.tokens) {
             const u32x4 n = *reinterpret_cast<const u32x4*>(cnt + j);
+            if (n.x | n.y | n.z | n.w)       // few entries have a history: most waves go past the divisions
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = apply_penalties(x[k], n[k], a.r);
+                for (int k = 0; k < 4; ++k) x[k] = apply_penalties(x[k], n[k], a.r);
         }
-        if (a.r.bias) {
-            const f32x4 bi = rules_load4(a.r.bias + lo + j, have - j);
+        if (a.r.bias)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = add_rn(x[k], bi[k]);
-        }
-        if (mask) {
-            const unsigned w = mask[(lo + j) >> 5] >> (j & 31);
+            for (int k = 0; k < 4; ++k) x[k] = add_rn(x[k], bi[i][k]);
+        if (mask)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = w >> k & 1u ? x[k] : -INFINITY;
-        }
+            for (int k = 0; k < 4; ++k) x[k] = w[i] >> (j & 31) >> k & 1u ? x[k] : -INFINITY;
         rules_store4(out + j, x, have - j);
     }
 }
