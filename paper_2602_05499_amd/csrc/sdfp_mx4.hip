@@ -19,24 +19,41 @@ int status(hipError_t e) { return e == hipSuccess ? SD_OK : SD_EHIP; }
 
 namespace sdfp {
 
-template <int XT>
-static void launch_rows(const Mx4Product& a, dim3 grid, hipStream_t s) {
-    if constexpr (XT == MX4_X_MX4) {
-        hipLaunchKernelGGL((k_mx4_rows<XT, 1>), grid, dim3(mx4_rows_waves(XT, 1) * 64), 0, s, a);
-    } else {
-    if (a.M == 1) hipLaunchKernelGGL((k_mx4_rows<XT, 1>), grid, dim3(mx4_rows_waves(XT, 1) * 64), 0, s, a);
-    else if (a.M <= 4) hipLaunchKernelGGL((k_mx4_rows<XT, 4>), grid, dim3(mx4_rows_waves(XT, 4) * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_mx4_rows<XT, 16>), grid, dim3(mx4_rows_waves(XT, 16) * 64), 0, s, a);
+// One launch of the kernel for a few rows.  A workgroup takes a panel of 64 outputs; one 16-row tile of it where that makes
+// too few workgroups (one row, 4096 outputs: 5.8 us against 6.9; 8192, 128 panels: equal; 11008: 9.3 against 8.0); two panels
+// where there are plenty and a row's cutting into pieces weighs (float32, 9 rows, 32000 outputs: 21.0 us against 25.8; for
+// one row two panels are slower, 16.4 against 15.3).
+template <int XT, int MP>
+static void launch_rows(const Mx4Product& a, hipStream_t s) {
+    const unsigned my = (unsigned)((a.M + 15) / 16), n_pan = (unsigned)mx4_row_panels(a.N);
+    const dim3 blk(MX4_WAVES * 64);
+    if (n_pan * my < 128) {
+        hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 1>), dim3(n_pan * 4 * my), blk, 0, s, a);
+        return;
     }
+    if constexpr (XT == MX4_X_F32 && MP >= 8)
+        if (n_pan * my >= 384) {
+            hipLaunchKernelGGL((k_mx4_rows<XT, MP, 2, 4>), dim3((n_pan + 1) / 2 * my), blk, 0, s, a);
+            return;
+        }
+    hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 4>), dim3(n_pan * my), blk, 0, s, a);
 }
 
 hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
-    const int64_t n = (int64_t)mx4_row_panels(a.N) * ((a.M + 15) / 16);
-    if (n > INT32_MAX) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)n);
-    if (a.x_type == MX4_X_F32) launch_rows<MX4_X_F32>(a, grid, stream);
-    else if (a.x_type == MX4_X_BF16) launch_rows<MX4_X_BF16>(a, grid, stream);
-    else launch_rows<MX4_X_MX4>(a, grid, stream);
+    if ((int64_t)mx4_row_panels(a.N) * (((int64_t)a.M + 15) / 16) > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (a.x_type == MX4_X_F32) {
+        if (a.M == 1) launch_rows<MX4_X_F32, 1>(a, stream);
+        else if (a.M <= 5) launch_rows<MX4_X_F32, 5>(a, stream);
+        else if (a.M <= 8) launch_rows<MX4_X_F32, 8>(a, stream);
+        else launch_rows<MX4_X_F32, 16>(a, stream);
+    } else if (a.x_type == MX4_X_BF16) {
+        if (a.M == 1) launch_rows<MX4_X_BF16, 1>(a, stream);
+        else if (a.M <= 4) launch_rows<MX4_X_BF16, 4>(a, stream);
+        else if (a.M <= 8) launch_rows<MX4_X_BF16, 8>(a, stream);
+        else launch_rows<MX4_X_BF16, 16>(a, stream);
+    } else {
+        launch_rows<MX4_X_MX4, 16>(a, stream);
+    }
     return hipGetLastError();
 }
 

@@ -151,16 +151,31 @@ __global__ __launch_bounds__(256) void k_mx4_dequantize(const char* __restrict__
     }
 }
 
-// A float32 value as three bfloat16 pieces by truncation, x = x0 + x1 + x2 exactly (8 bits of the significand each; what is
-// below the smallest bfloat16 is lost); the pieces' bits lie in the upper halves.  Truncation keeps the first piece of a large
-// finite value finite; an infinity is its first piece alone, a NaN stays NaN.
-__device__ __forceinline__ void trunc3(float x, unsigned (&p)[3]) {
-    p[0] = __float_as_uint(x) & 0xFFFF0000u;
-    float r = sub_rn(x, __uint_as_float(p[0]));
-    if (p[0] << 1 == 0xFF000000u) r = __float_as_uint(x) == p[0] ? 0.f : x;   // infinity; NaN whose payload was cut off
-    p[1] = __float_as_uint(r) & 0xFFFF0000u;
-    p[2] = __float_as_uint(sub_rn(r, __uint_as_float(p[1]))) & 0xFFFF0000u;
-    if (x != x) p[0] = 0x7FC00000u;
+// Float32 values as three bfloat16 pieces by truncation, x = x0 + x1 + x2 exactly (8 bits of the significand each; what is
+// below the smallest bfloat16 is lost): pk[p][i] holds piece p of values 2 i and 2 i + 1.  Truncation keeps the first piece of
+// a large finite value finite; an infinity is its first piece alone, a NaN stays one.
+template <int N>
+__device__ __forceinline__ void trunc3(const float (&x)[N], unsigned (&pk)[3][N / 2]) {
+    auto hi = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
+    auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };   // upper halves
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const float a = x[2 * i], b = x[2 * i + 1];
+        const float ra = sub_rn(a, hi(a)), rb = sub_rn(b, hi(b));
+        odd |= __builtin_isunordered(ra, rb);      // an infinity or a NaN left a NaN
+        pk[0][i] = pair(a, b);
+        pk[1][i] = pair(ra, rb);
+        pk[2][i] = pair(sub_rn(ra, hi(ra)), sub_rn(rb, hi(rb)));
+    }
+    if (odd)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const unsigned half = e % 2 ? 0xFFFF0000u : 0x0000FFFFu;
+            if ((__float_as_uint(x[e]) & 0x7F800000u) != 0x7F800000u) continue;
+            if (x[e] != x[e]) pk[0][e / 2] = (pk[0][e / 2] & ~half) | (0x7FC07FC0u & half);
+            pk[1][e / 2] &= ~half; pk[2][e / 2] &= ~half;
+        }
 }
 
 // 8 values of a block -- the codes of one word -- as a bfloat16 matrix-core operand, scale applied (exact)
@@ -190,36 +205,52 @@ __device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_
     }
 }
 
-// ---- product of a few rows: bound by the read of the panels.  A workgroup computes one panel's 64 outputs for 16 rows of x,
-// its waves split the reduction dimension by panels and add their sums in wave order at the end.  The panel's codes go from
-// memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies the
-// 8 values of word j), x into the B operand with the same permutation of columns.  float32 x runs as three exact bfloat16
-// pieces, in MXFP4 as it is on the scaled 4-bit instruction.  MP: rows of x that are staged (a power of two; lanes of the
-// operand past them read the same values again, their columns are not stored).
-// W: waves of the workgroup, as many as the staged rows leave room for in 64 KB of LDS.
-constexpr int mx4_rows_waves(int xt, int mp) { return xt == MX4_X_F32 && mp == 16 ? 4 : 8; }
-template <int XT, int MP>
-__global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Product a) {
-    constexpr int W = mx4_rows_waves(XT, MP);
-    constexpr int NPC = XT == MX4_X_F32 ? 3 : 1;
-    constexpr int STAGE = XT == MX4_X_MX4 ? 0 : NPC * 16 * MP * 16;          // bytes of a wave's staged panel of x
-    constexpr int RED = W * 4 * 64 * 16;
+// ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head 15.4 us, 4.5 TB/s with the launch's
+// ends; 128256 x 4096 49.5 us, 5.7 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
+// for 16 rows of x; its waves split the reduction dimension by panels and add their sums in wave order at the end.  The codes
+// go from memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies
+// the 8 values of word j), one panel ahead -- two to four ahead were slower, 17.7 to 23 us --, x through a few kilobytes of LDS
+// that belong to the wave into the B operand, in the same order of columns.  x in MXFP4 goes as it is into the scaled 4-bit
+// instruction; float32 x is cut into three exact bfloat16 pieces, which take three of the operand's 16 columns for each row
+// while rows are few (MP <= 5: one instruction where three would run; 17.7 -> 15.5 us) and three instructions otherwise.  MP:
+// rows of x that are staged; lanes of the operand past them read values whose results are dropped.
+constexpr bool mx4_rows_in_columns(int xt, int mp) { return xt == MX4_X_F32 && mp <= 5; }
+constexpr int MX4_WAVES = 8;
+template <int XT, int MP, int NPAN, int TT>
+__global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
+    constexpr int W = MX4_WAVES;
+    constexpr bool COLS = mx4_rows_in_columns(XT, MP);
+    constexpr int NPC = XT == MX4_X_F32 ? 3 : 1;                             // pieces of a value
+    constexpr int NI = COLS ? 1 : NPC;                                       // instructions per sub-step and tile
+    // the staged panel of x, one piece after the other (or with the pieces as columns): 16 entries -- sub-step j, block b -- of
+    // 16 bytes per column, a multiple of 16 bytes apart that is no power of two, so that the lanes of a row write to different
+    // banks
+    constexpr int COLUMNS = COLS ? 3 * MP : MP;
+    constexpr int ENTRY = (COLUMNS % 2 ? COLUMNS : COLUMNS + 1) * 16;
+    constexpr int STAGE = XT == MX4_X_MX4 ? 0 : 16 * ENTRY;                 // bytes, each wave's own
+    constexpr int RED = W * TT * 64 * 16;
     __shared__ __attribute__((aligned(16))) char sh[W * STAGE > RED ? W * STAGE : RED];
     __shared__ float s_sq[W][16];
-    __shared__ unsigned s_bad_n[MX4_ROWS], s_bad_m[16];
+    __shared__ unsigned s_bad_n[NPAN * MX4_ROWS], s_bad_m[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
-    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS;
-    const int my = (a.M + 15) / 16, panel = blockIdx.x / my;
+    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS, n_pan = (a.N + MX4_ROWS - 1) / MX4_ROWS;
+    const int my = (a.M + 15) / 16, unit = blockIdx.x / my;
+    const int panel0 = NPAN > 1 ? unit * NPAN : unit / (4 / TT), t0 = NPAN > 1 ? 0 : unit % (4 / TT) * TT;
     const int64_t m0 = (int64_t)(blockIdx.x % my) * 16;
-    const char* wp = a.w + (size_t)panel * kps * MX4_PANEL_BYTES;
-    if (tid < MX4_ROWS) s_bad_n[tid] = 0;
+    for (int i = tid; i < NPAN * MX4_ROWS; i += W * 64) s_bad_n[i] = 0;
     if (tid < 16) s_bad_m[tid] = 0;
     __syncthreads();
 
-    f32x4 acc[4];
+    const char* wp[NPAN];                                                    // (panels past the end repeat the last one)
+    f32x4 acc[NPAN][TT];
+    unsigned bad[NPAN], bad_x = 0;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    unsigned bad = 0, bad_x = 0;
+    for (int q = 0; q < NPAN; ++q) {
+        wp[q] = a.w + (size_t)min(panel0 + q, n_pan - 1) * kps * MX4_PANEL_BYTES;
+        bad[q] = 0;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     constexpr int VE = XT == MX4_X_F32 ? 4 : 8;
     constexpr int PER_ROW = MX4_COLS / VE;                                   // lanes per row of a staged panel
     constexpr int NL = XT == MX4_X_MX4 ? 1 : (MP * PER_ROW + 63) / 64;       // loads per lane
@@ -227,13 +258,17 @@ __global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Pro
 #pragma unroll
     for (int i = 0; i < NL; ++i) sq[i] = 0.f;
     char* stage = sh + wave * STAGE;
+    const int col = COLS ? min(c16, COLUMNS - 1) : c16 & (MP - 1);
 
-    struct Load { u32x4 code[4]; unsigned scale; u32x4 x[NL]; u32x4 gain; };
+    struct Load { u32x4 code[NPAN][TT]; unsigned scale[NPAN]; u32x4 x[NL]; u32x4 gain; };
     auto fetch = [&](int kp, Load& L, bool tail) {
-        const char* p = wp + (size_t)kp * MX4_PANEL_BYTES + lane * 16;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) L.code[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(p + t * MX4_TILE_BYTES));
-        L.scale = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(p + MX4_CODE_BYTES - lane * 12));
+        for (int q = 0; q < NPAN; ++q) {
+            const char* p = wp[q] + (size_t)kp * MX4_PANEL_BYTES;
+#pragma unroll
+            for (int t = 0; t < TT; ++t) L.code[q][t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(p + (t0 + t) * MX4_TILE_BYTES + lane * 16));
+            L.scale[q] = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(p + MX4_CODE_BYTES + lane * 4)) >> (8 * t0);
+        }
         if constexpr (XT == MX4_X_MX4) {
             const char* xp = (const char*)a.x + ((size_t)(m0 / MX4_ROWS) * kps + kp) * MX4_PANEL_BYTES;
             const int t = (int)(m0 / 16) & 3;
@@ -252,18 +287,28 @@ __global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Pro
         }
     };
     auto multiply = [&](const Load& L) {
-        bad |= mx4_nan_bytes(L.scale);
         if constexpr (XT == MX4_X_MX4) {
             bad_x |= L.gain.x == 255u;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = mx4_mfma(L.code[t], (int)(L.scale >> (8 * t)), L.x[0], (int)L.gain.x, acc[t]);
-        } else {
-            // x of this panel into LDS: piece p, sub-step j, block b, row m at (((p * 4 + j) * 4 + b) * MP + m) * 16
+            for (int q = 0; q < NPAN; ++q) {
+                bad[q] |= mx4_nan_bytes(L.scale[q]);
 #pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int m = (i * 64 + lane) / PER_ROW, cc = (lane % PER_ROW) * VE, b = cc / 32, j = cc % 32 / 8;
-                char* to = stage + ((j * 4 + b) * MP + m) * 16;
-                if constexpr (XT == MX4_X_F32) {
+                for (int t = 0; t < TT; ++t) acc[q][t] = mx4_mfma(L.code[q][t], (int)(L.scale[q] >> (8 * t)), L.x[0], (int)L.gain.x, acc[q][t]);
+            }
+        } else {
+            bf16x8 xb[4][NI];
+            auto at = [&](int i) { const int cc = (lane % PER_ROW) * VE; return stage + (cc % 32 / 8 * 4 + cc / 32) * ENTRY + (i * 64 + lane) / PER_ROW * 16; };
+            auto staged = [&](int i) { return MP * PER_ROW % 64 == 0 || (i * 64 + lane) / PER_ROW < MP; };
+            auto take = [&](int p) {
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xb[j][p] = *reinterpret_cast<const bf16x8*>(stage + (j * 4 + g) * ENTRY + col * 16);
+                __builtin_amdgcn_wave_barrier();
+            };
+            if constexpr (XT == MX4_X_F32) {
+                unsigned pk[NL][3][2];
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
                     float v[4], gn[4];
                     Mx4In<XT>::unpack(L.x[i], v);
                     if (a.gain) {
@@ -271,57 +316,57 @@ __global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Pro
 #pragma unroll
                         for (int e = 0; e < 4; ++e) { sq[i] = fmaf(v[e], v[e], sq[i]); v[e] *= gn[e]; }
                     }
-                    unsigned pc[4][3];
+                    trunc3(v, pk[i]);
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) trunc3(v[e], pc[e]);
-                    if (m < MP)
+                for (int p = 0; p < 3; ++p) {
 #pragma unroll
-                        for (int p = 0; p < 3; ++p)
-                            *reinterpret_cast<u32x2*>(to + p * 16 * MP * 16 + cc % 8 * 2) =
-                                u32x2{pc[0][p] >> 16 | pc[1][p], pc[2][p] >> 16 | pc[3][p]};
-                } else {
-                    if (m < MP) *reinterpret_cast<u32x4*>(to) = L.x[i];
+                    for (int i = 0; i < NL; ++i)
+                        if (staged(i)) *reinterpret_cast<u32x2*>(at(i) + (COLS ? p * MP * 16 : 0) + lane % 2 * 8) = u32x2{pk[i][p][0], pk[i][p][1]};
+                    if (!COLS) take(p);
+                }
+                if (COLS) take(0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    if (staged(i)) *reinterpret_cast<u32x4*>(at(i)) = L.x[i];
+                take(0);
+            }
+#pragma unroll
+            for (int q = 0; q < NPAN; ++q) {
+                bad[q] |= mx4_nan_bytes(L.scale[q]);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    const unsigned e = L.scale[q] >> (8 * t) & 255u;
+                    const float s = __uint_as_float(e == 0u ? 0x00400000u : e << 23);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const bf16x8 wb = mx4_decode(L.code[q][t][j], s);
+#pragma unroll
+                        for (int p = 0; p < NI; ++p) acc[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[j][p], acc[q][t], 0, 0, 0);
+                    }
                 }
             }
-            __builtin_amdgcn_wave_barrier();
-            float s[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const unsigned e = L.scale >> (8 * t) & 255u;
-                s[t] = __uint_as_float(e == 0u ? 0x00400000u : e << 23);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bf16x8 xb[NPC];
-#pragma unroll
-                for (int p = 0; p < NPC; ++p)
-                    xb[p] = *reinterpret_cast<const bf16x8*>(stage + (((p * 4 + j) * 4 + g) * MP + (c16 & (MP - 1))) * 16);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const bf16x8 wb = mx4_decode(L.code[t][j], s[t]);
-#pragma unroll
-                    for (int p = 0; p < NPC; ++p) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[p], acc[t], 0, 0, 0);
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
         }
     };
 
     const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
-    Load cur, nxt;
-    if (wave < full) fetch(wave, cur, false);
+    Load nxt;                                                                // one panel ahead
+    if (wave < full) fetch(wave, nxt, false);
     for (int kp = wave; kp < full; kp += W) {
+        const Load cur = nxt;
         if (kp + W < full) fetch(kp + W, nxt, false);
         multiply(cur);
-        cur = nxt;
     }
-    if (full < kps && full % W == wave) { fetch(full, cur, true); multiply(cur); }
+    if (full < kps && full % W == wave) { fetch(full, nxt, true); multiply(nxt); }
 
-    // sums of the waves, in wave order
-    if (bad)
+    // the waves' sums, in wave order (and the pieces' after one another), a panel at a time
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-            if (bad >> (8 * t) & 128u) s_bad_n[t * 16 + c16] = 1u;
+    for (int q = 0; q < NPAN; ++q)
+        if (bad[q])
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+                if (bad[q] >> (8 * t) & 128u) s_bad_n[q * MX4_ROWS + t * 16 + c16] = 1u;
     if (bad_x) s_bad_m[c16] = 1u;
     if constexpr (XT == MX4_X_F32)
         if (a.gain)
@@ -333,35 +378,39 @@ __global__ __launch_bounds__(mx4_rows_waves(XT, MP) * 64) void k_mx4_rows(Mx4Pro
                 const int m = (i * 64 + lane) / PER_ROW;
                 if (lane % 32 == 0 && m < 16) s_sq[wave][m] = v;
             }
-    __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(sh + ((wave * 4 + t) * 64 + lane) * 16) = acc[t];
-    __syncthreads();
-    if (tid >= 256) return;
-    f32x4 y = *reinterpret_cast<const f32x4*>(sh + tid * 16);
+    for (int q = 0; q < NPAN; ++q) {
+        __syncthreads();
 #pragma unroll
-    for (int w = 1; w < W; ++w) {
-        const f32x4 o = *reinterpret_cast<const f32x4*>(sh + (w * 256 + tid) * 16);
-        y.x += o.x; y.y += o.y; y.z += o.z; y.w += o.w;
+        for (int t = 0; t < TT; ++t) *reinterpret_cast<f32x4*>(sh + ((wave * TT + t) * 64 + lane) * 16) = acc[q][t];
+        __syncthreads();
+        const int64_t m = m0 + c16;
+        const int nr = (tid >> 6) * 16 + g * 4;
+        const int64_t n = (int64_t)(panel0 + q) * MX4_ROWS + t0 * 16 + nr;
+        if (tid >= TT * 64 || c16 >= MP || m >= a.M || n >= a.N) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < (COLS ? 3 : 1); ++p)
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const f32x4 o = *reinterpret_cast<const f32x4*>(sh + (w * TT * 64 + tid + p * MP) * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += o[i];
+            }
+        if constexpr (XT == MX4_X_F32)
+            if (a.gain) {
+                float ss = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) ss += s_sq[w][c16];
+                const float rs = rms_recip(ss, a.K, a.eps);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] *= rs;
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s_bad_n[q * MX4_ROWS + nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
+        mx4_store(a, m, n, v);
     }
-    const int64_t m = m0 + c16;
-    const int nr = (tid >> 6) * 16 + g * 4;
-    const int64_t n = (int64_t)panel * MX4_ROWS + nr;
-    if (m >= a.M || n >= a.N) return;
-    float v[4] = {y.x, y.y, y.z, y.w};
-    if constexpr (XT == MX4_X_F32)
-        if (a.gain) {
-            float ss = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) ss += s_sq[w][c16];
-            const float rs = rms_recip(ss, a.K, a.eps);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= rs;
-        }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (s_bad_n[nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
-    mx4_store(a, m, n, v);
 }
 
 }  // namespace sdfp
