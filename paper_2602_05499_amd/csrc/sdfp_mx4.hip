@@ -2,13 +2,15 @@
 #include "sdfp_mx4.hip.h"
 #include "sdfp.h"
 
+#include <atomic>
+
 using namespace sdfp;
 
 static_assert(SD_F32 == MX4_X_F32 && SD_BF16 == MX4_X_BF16 && SD_MX4 == MX4_X_MX4, "type codes");
 
 namespace {
 bool row_type(int t) { return t == SD_F32 || t == SD_BF16; }
-bool size_ok(int rows, int cols) { return rows >= 1 && cols >= 1 && cols <= INT32_MAX - MX4_COLS; }
+bool size_ok(int rows, int cols) { return rows >= 1 && cols >= 1 && rows <= INT32_MAX - 1024 && cols <= INT32_MAX - 1024; }   // (sizes are rounded up in int)
 // panels of a matrix, as the grid of a launch: SD_EINVAL past what a launch can hold
 bool grid_ok(int rows, int cols) { return (int64_t)mx4_row_panels(rows) * mx4_col_panels(cols) <= INT32_MAX; }
 bool rows_ok(const void* x, int type, int64_t ld, int cols) {
@@ -39,19 +41,74 @@ static void launch_rows(const Mx4Product& a, hipStream_t s) {
     hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 4>), dim3(n_pan * my), blk, 0, s, a);
 }
 
+// A kernel's dynamic LDS limit, raised once per device.
+static hipError_t raise_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    if ((e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) == hipSuccess) done.fetch_or(bit);
+    return e;
+}
+template <int XT, int CT, int WN, int WM, int KW>
+static hipError_t launch_tiles(const Mx4Product& a, hipStream_t s) {
+    typedef Mx4Tile<XT, CT, WN, WM, KW> S;
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = raise_lds(reinterpret_cast<const void*>(k_mx4_tiles<XT, CT, WN, WM, KW>), S::LDS, done);
+    if (e != hipSuccess) return e;
+    const int64_t n = (int64_t)((mx4_row_panels(a.N) + WN - 1) / WN) * ((a.M + S::TM - 1) / S::TM);
+    hipLaunchKernelGGL((k_mx4_tiles<XT, CT, WN, WM, KW>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(S::THREADS), S::LDS, s, a);
+    return hipGetLastError();
+}
+template <int CT, int WN, int WM>
+static hipError_t launch_tiles_mx4(const Mx4Product& a, hipStream_t s) {
+    typedef Mx4TileX<CT, WN, WM> S;
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = raise_lds(reinterpret_cast<const void*>(k_mx4_tiles_mx4<CT, WN, WM>), S::LDS, done);
+    if (e != hipSuccess) return e;
+    const int64_t n = (int64_t)((mx4_row_panels(a.N) + WN - 1) / WN) * ((mx4_row_panels(a.M) + S::XP - 1) / S::XP);
+    hipLaunchKernelGGL((k_mx4_tiles_mx4<CT, WN, WM>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(64 * S::WAVES), S::LDS, s, a);
+    return hipGetLastError();
+}
+
+// Which kernel: the one for a few rows while its workgroups' 16-row by 64-output pieces are few (each reads the codes and
+// cuts the rows up anew), a small tile whose waves split the reduction while those make a round of the 256 compute units or two, a middle one
+// for the next round, the large tile from there on.  Microseconds, K 4096 (few rows / small / middle / large):
+//   bfloat16  128 x 4096 14/16/31/48, 64 x 11008 18/17/33/49, 512 x 4096 33/31/32/48, 256 x 11008 46/44/32/49, 512 x 11008 87/82/60/50,
+//             4096 x 14336 849/771/455/375 (1.28 PFLOP/s; the library's bfloat16 product of that size 396)
+//   float32   128 x 4096 23/46/52/126, 512 x 4096 72/52/57/127, 256 x 11008 99/91/83/128, 2048 x 4096 256/183/161/137,
+//             4096 x 14336 1801/1288/1108/972 (three products: 1.48 PFLOP/s)
+//   MXFP4     128 x 4096 13/15/-/25, 256 x 11008 30/20/-/27, 2048 x 4096 62/29/-/29, 4096 x 14336 413/222/-/164 (2.9 PFLOP/s)
 hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
-    if ((int64_t)mx4_row_panels(a.N) * (((int64_t)a.M + 15) / 16) > INT32_MAX) return hipErrorInvalidConfiguration;
+    const int64_t n_pan = mx4_row_panels(a.N), pieces = n_pan * (((int64_t)a.M + 15) / 16);
+    if (pieces > INT32_MAX) return hipErrorInvalidConfiguration;
+    auto tiles = [&](int n, int m) { return (((int64_t)a.N + n - 1) / n) * (((int64_t)a.M + m - 1) / m); };
     if (a.x_type == MX4_X_F32) {
+        if (a.M > 16 && pieces > 1400) {
+            if (tiles(256, 32) <= 256) return launch_tiles<MX4_X_F32, 2, 4, 1, 2>(a, stream);
+            if (tiles(256, 32) <= 512) return launch_tiles<MX4_X_F32, 2, 4, 1, 1>(a, stream);
+            return launch_tiles<MX4_X_F32, 4, 8, 1, 1>(a, stream);
+        }
         if (a.M == 1) launch_rows<MX4_X_F32, 1>(a, stream);
         else if (a.M <= 5) launch_rows<MX4_X_F32, 5>(a, stream);
         else if (a.M <= 8) launch_rows<MX4_X_F32, 8>(a, stream);
         else launch_rows<MX4_X_F32, 16>(a, stream);
     } else if (a.x_type == MX4_X_BF16) {
+        if (a.M > 16 && pieces > 600) {
+            if (tiles(128, 32) <= 512) return launch_tiles<MX4_X_BF16, 2, 2, 1, 4>(a, stream);
+            if (tiles(256, 64) <= 256) return launch_tiles<MX4_X_BF16, 4, 4, 1, 2>(a, stream);
+            return launch_tiles<MX4_X_BF16, 4, 8, 1, 1>(a, stream);
+        }
         if (a.M == 1) launch_rows<MX4_X_BF16, 1>(a, stream);
         else if (a.M <= 4) launch_rows<MX4_X_BF16, 4>(a, stream);
         else if (a.M <= 8) launch_rows<MX4_X_BF16, 8>(a, stream);
         else launch_rows<MX4_X_BF16, 16>(a, stream);
     } else {
+        if (a.M > 16 && pieces > 768) {
+            if (tiles(256, 128) < 256) return launch_tiles_mx4<4, 2, 1>(a, stream);
+            return launch_tiles_mx4<8, 4, 1>(a, stream);
+        }
         launch_rows<MX4_X_MX4, 16>(a, stream);
     }
     return hipGetLastError();
@@ -88,7 +145,7 @@ int sd_mx4_dequantize(const void* q, size_t q_bytes, int32_t rows, int32_t cols,
 
 int sd_mx4_matmul(const void* w, size_t w_bytes, int32_t N, int32_t K, const void* x, int x_dtype, int64_t ldx, int32_t M,
                   const float* gain, float eps, void* y, int y_dtype, int64_t ldy, void* hip_stream) {
-    if (!size_ok(N, K) || M < 1 || !grid_ok(N, K) || !w || ((uintptr_t)w & 255) || !rows_ok(y, y_dtype, ldy, N)) return SD_EINVAL;
+    if (!size_ok(N, K) || !size_ok(M, K) || !grid_ok(N, K) || !w || ((uintptr_t)w & 255) || !rows_ok(y, y_dtype, ldy, N)) return SD_EINVAL;
     if (x_dtype == SD_MX4 ? !x || ((uintptr_t)x & 255) || ldx < 0 || !grid_ok(M, K) : !rows_ok(x, x_dtype, ldx, K)) return SD_EINVAL;
     if (gain && (x_dtype != SD_F32 || ((uintptr_t)gain & 3) || !(eps >= 0.f))) return SD_EINVAL;
     if (w_bytes < mx4_bytes(N, K) || (x_dtype == SD_MX4 && (size_t)ldx < mx4_bytes(M, K))) return SD_ENOMEM;

@@ -258,6 +258,7 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) sq[i] = 0.f;
     char* stage = sh + wave * STAGE;
+    const float* gain = a.gain ? a.gain : (const float*)a.x;                 // (without a gain: loaded, not used)
     const int col = COLS ? min(c16, COLUMNS - 1) : c16 & (MP - 1);
 
     struct Load { u32x4 code[NPAN][TT]; unsigned scale[NPAN]; u32x4 x[NL]; u32x4 gain; };
@@ -282,8 +283,7 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
                 const int64_t row = min(m0 + min((i * 64 + lane) / PER_ROW, MP - 1), (int64_t)a.M - 1);
                 L.x[i] = mx4_load<XT>((const T*)a.x + row * a.ldx, k, a.K, !tail);
             }
-            if constexpr (XT == MX4_X_F32)
-                if (a.gain) L.gain = mx4_load<XT>(a.gain, k, a.K, !tail);
+            if constexpr (XT == MX4_X_F32) L.gain = mx4_load<XT>(gain, k, a.K, !tail);
         }
     };
     auto multiply = [&](const Load& L) {
@@ -351,11 +351,13 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
     };
 
     const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
-    Load nxt;                                                                // one panel ahead
+    // One panel ahead.  Every load of the loop is unconditional (past the end the last panel once more): behind a load under a
+    // condition the compiler waits for everything in flight, the panel ahead included.
+    Load nxt;
     if (wave < full) fetch(wave, nxt, false);
     for (int kp = wave; kp < full; kp += W) {
         const Load cur = nxt;
-        if (kp + W < full) fetch(kp + W, nxt, false);
+        fetch(min(kp + W, full - 1), nxt, false);
         multiply(cur);
     }
     if (full < kps && full % W == wave) { fetch(full, nxt, true); multiply(nxt); }
@@ -410,6 +412,342 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
         for (int i = 0; i < 4; ++i)
             if (s_bad_n[q * MX4_ROWS + nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
         mx4_store(a, m, n, v);
+    }
+}
+
+// ---- product of many rows: bound by the matrix cores.  A workgroup of WN x WM x KW waves computes WN panels of 64 outputs for
+// 16 CT WM rows of x, a wave one panel for 16 CT rows over every KW-th 128 columns (their sums are added at the end: with few
+// tiles it takes several waves per SIMD to hide what a step waits for).  x goes through LDS (as bfloat16 pieces, two buffers, the
+// columns of the next two steps on their way in registers), in operand order: the operand of 16 rows and sub-step j is a
+// kilobyte of which lane l = 16 b + r reads its 16 bytes at l * 16, free of bank conflicts however the hardware groups the lanes.  A wave
+// stages a quarter of each block (sub-step) at a time: lane 16 g + r brings columns 32 i + 8 g .. of row r.  The codes go straight into
+// the wave's registers and are turned into bfloat16 operands there: 64 conversions for 64 CT matrix instructions per piece.
+template <int XT, int CT, int WN, int WM, int KW>
+struct Mx4Tile {
+    static constexpr int THREADS = 64 * WN * WM * KW, TM = 16 * CT * WM, NPC = XT == MX4_X_F32 ? 3 : 1;
+    static constexpr int PANEL = NPC * TM * 256, BUF = KW * PANEL; // bytes of x: 128 columns, a step
+    static constexpr int RED = (KW - 1) * WN * WM * 64 * 16 * CT * 4;
+    static constexpr int LDS = 2 * BUF > RED ? 2 * BUF : RED;
+    static constexpr int WAVES = WN * WM * KW;
+    static constexpr int PER_K = TM / 4 / WAVES, NCH = KW * PER_K; // 8-element pieces of x that a thread stages: of 128 columns, in all
+    static constexpr int AHEAD = NPC == 3 ? 2 : 4;                 // units whose operands are read ahead
+    static_assert(TM / 4 % WAVES == 0 && WAVES % 4 == 0, "a wave stages one block of the columns of some row tiles");
+};
+// Workgroup -> tile of n_n x n_m: workgroups run on XCD id % 8, each XCD takes a stretch of tiles of its own, and a stretch
+// goes through the outputs for 8 row tiles at a time, row tiles fastest: its L2 sees the same codes and rows again soon.
+__device__ __forceinline__ bool mx4_tile_of(int n_n, int n_m, int& n, int& m) {
+    const int per = (n_n * n_m + 7) / 8, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || tile >= n_n * n_m) return false;
+    const int group = tile / (8 * n_n), r = tile - group * 8 * n_n, in = min(8, n_m - group * 8);
+    n = r / in; m = group * 8 + r % in;
+    return true;
+}
+// which of a tile's 16 weight rows have a NaN block, by the high bits that mx4_nan_bytes found (bit t of every byte's lane)
+__device__ __forceinline__ unsigned mx4_nan_rows(unsigned bad, int t) {
+    const unsigned long long v = __ballot(bad >> (8 * t) & 128u);
+    return (unsigned)(v | v >> 16 | v >> 32 | v >> 48) & 0xFFFFu;
+}
+template <int XT, int CT, int WN, int WM, int KW>
+__global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a) {
+    typedef Mx4Tile<XT, CT, WN, WM, KW> S;
+    typedef typename Mx4In<XT>::T T;
+    extern __shared__ __attribute__((aligned(16))) char sh[];
+    __shared__ float s_sq[KW * 4][S::TM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+    const int wn = wave % WN, wm = wave / WN % WM, kg = wave / (WN * WM);
+    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS, steps = (kps + KW - 1) / KW, n_pan = (a.N + MX4_ROWS - 1) / MX4_ROWS;
+    int tn, tm;
+    if (!mx4_tile_of((n_pan + WN - 1) / WN, (a.M + S::TM - 1) / S::TM, tn, tm)) return;
+    const int panel = tn * WN + wn;
+    const int64_t m0 = (int64_t)tm * S::TM;
+    const char* wp = a.w + (size_t)min(panel, n_pan - 1) * kps * MX4_PANEL_BYTES;
+    constexpr int XV = XT == MX4_X_F32 ? 2 : 1;
+    // what this wave stages: block wave % 4 of the columns, sub-step g, of row tiles wave / 4, + WAVES / 4 ..
+    const int blk = wave % 4, tile0 = wave / 4;
+
+    struct Load { u32x4 x[S::NCH][XV], gain[KW][XV], code[4]; unsigned scale; };   // what a step brings, on its way
+    Load f0, f1;
+    unsigned bad = 0;
+    float sq[S::NCH];
+    f32x4 acc[4][CT];
+#pragma unroll
+    for (int i = 0; i < S::NCH; ++i) sq[i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const T* xrow[S::PER_K];
+#pragma unroll
+    for (int i = 0; i < S::PER_K; ++i) xrow[i] = (const T*)a.x + min(m0 + (tile0 + i * (S::WAVES / 4)) * 16 + c16, (int64_t)a.M - 1) * a.ldx;
+    const float* gain = a.gain ? a.gain : (const float*)a.x;       // (without a gain: loaded, not used)
+    auto fetch = [&](int st, Load& f, bool full) {
+        const char* p = wp + (size_t)min(st * KW + kg, kps - 1) * MX4_PANEL_BYTES;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) f.code[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(p + t * MX4_TILE_BYTES + lane * 16));
+        f.scale = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(p + MX4_CODE_BYTES + lane * 4));
+#pragma unroll
+        for (int z = 0; z < KW; ++z) {
+            const int64_t k = (int64_t)(st * KW + z) * MX4_COLS + blk * 32 + g * 8;
+#pragma unroll
+            for (int v = 0; v < XV; ++v) {
+#pragma unroll
+                for (int i = 0; i < S::PER_K; ++i) f.x[z * S::PER_K + i][v] = mx4_load<XT>(xrow[i], k + v * 4, a.K, full);
+                if constexpr (XT == MX4_X_F32) f.gain[z][v] = mx4_load<XT>(gain, k + v * 4, a.K, full);
+            }
+        }
+    };
+    auto store_x = [&](const Load& f, char* buf) {
+#pragma unroll
+        for (int i = 0; i < S::NCH; ++i) {
+            char* to = buf + i / S::PER_K * S::PANEL + ((tile0 + i % S::PER_K * (S::WAVES / 4)) * 4 + g) * 1024 + (blk * 16 + c16) * 16;
+            if constexpr (XT == MX4_X_F32) {
+                float v[8], gn[8];
+                Mx4In<XT>::unpack(f.x[i][0], *reinterpret_cast<float(*)[4]>(v));
+                Mx4In<XT>::unpack(f.x[i][1], *reinterpret_cast<float(*)[4]>(v + 4));
+                if (a.gain) {
+                    Mx4In<XT>::unpack(f.gain[i / S::PER_K][0], *reinterpret_cast<float(*)[4]>(gn));
+                    Mx4In<XT>::unpack(f.gain[i / S::PER_K][1], *reinterpret_cast<float(*)[4]>(gn + 4));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { sq[i] = fmaf(v[e], v[e], sq[i]); v[e] *= gn[e]; }
+                }
+                unsigned pk[3][4];
+                trunc3(v, pk);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(to + p * S::TM * 256) = u32x4{pk[p][0], pk[p][1], pk[p][2], pk[p][3]};
+            } else {
+                *reinterpret_cast<u32x4*>(to) = f.x[i][0];
+            }
+        }
+    };
+    auto multiply = [&](const char* buf, const u32x4 (&code)[4], unsigned scale) {
+        buf += kg * S::PANEL + wm * CT * 4096 + lane * 16;
+        bad |= mx4_nan_bytes(scale);
+        float s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const unsigned e = scale >> (8 * t) & 255u;
+            s[t] = __uint_as_float(e == 0u ? 0x00400000u : e << 23);
+        }
+        // unit u: sub-step u / CT, row tile u % CT; its operands are read S::AHEAD units earlier, and while a sub-step's units
+        // run the weights of the next are decoded, a few tiles per unit
+        bf16x8 xb[S::AHEAD][S::NPC], wb[2][4];
+        auto read = [&](int u) {
+#pragma unroll
+            for (int p = 0; p < S::NPC; ++p)
+                xb[u % S::AHEAD][p] = *reinterpret_cast<const bf16x8*>(buf + p * S::TM * 256 + (u % CT * 4 + u / CT) * 1024);
+        };
+#pragma unroll
+        for (int u = 0; u < S::AHEAD; ++u) read(u);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) wb[0][t] = mx4_decode(code[t][0], s[t]);
+#pragma unroll
+        for (int u = 0; u < 4 * CT; ++u) {
+            const int j = u / CT, c = u % CT;
+#pragma unroll
+            for (int p = 0; p < S::NPC; ++p)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j & 1][t], xb[u % S::AHEAD][p], acc[t][c], 0, 0, 0);
+            if (u + S::AHEAD < 4 * CT) read(u + S::AHEAD);
+            if (j < 3)
+#pragma unroll
+                for (int t = 4 * c / CT; t < 4 * (c + 1) / CT; ++t) wb[~j & 1][t] = mx4_decode(code[t][j + 1], s[t]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Step st: x lies in LDS, the codes in f, which is then free for step st + 2; next, on its way since the step before, goes to LDS.
+    // Every load of the loop is unconditional (past the end the last step once more): behind a load under a condition the
+    // compiler waits for everything in flight.
+    const int full = a.K / (MX4_COLS * KW);                        // steps without a ragged end
+    auto step = [&](int st, Load& f, const Load& next) {
+        u32x4 code[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) code[t] = f.code[t];
+        const unsigned scale = f.scale;
+        fetch(min(st + 2, full - 1), f, true);
+        multiply(sh + (st & 1) * S::BUF, code, scale);
+        if (st + 1 < full) store_x(next, sh + (~st & 1) * S::BUF);
+        __syncthreads();
+    };
+    if (full > 0) {
+        fetch(0, f0, true);
+        fetch(min(1, full - 1), f1, true);
+        store_x(f0, sh);
+        __syncthreads();
+        int st = 0;
+        for (; st + 1 < full; st += 2) { step(st, f0, f1); step(st + 1, f1, f0); }
+        if (st < full) step(st, f0, f1);
+    }
+    if (full < steps) {
+        fetch(full, f0, false);
+        store_x(f0, sh);
+        __syncthreads();
+        if (full * KW + kg < kps) multiply(sh, f0.code, f0.scale);
+        __syncthreads();
+    }
+    if constexpr (XT == MX4_X_F32)
+        if (a.gain)
+#pragma unroll
+            for (int i = 0; i < S::NCH; ++i) {
+                float v = sq[i];
+                v += __shfl_xor(v, 16);
+                v += __shfl_xor(v, 32);
+                if (g == 0) s_sq[i / S::PER_K * 4 + blk][(tile0 + i % S::PER_K * (S::WAVES / 4)) * 16 + c16] = v;
+            }
+    __shared__ unsigned s_bad[KW > 1 ? S::THREADS : 1];
+    if constexpr (KW > 1) {   // the other waves' sums of this tile, in their order
+        f32x4* red = reinterpret_cast<f32x4*>(sh);
+        if (kg > 0) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) red[((wave - WN * WM) * 4 * CT + t * CT + c) * 64 + lane] = acc[t][c];
+        }
+        s_bad[tid] = bad;
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int z = 1; z < KW; ++z) {
+            bad |= s_bad[tid + z * WN * WM * 64];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const f32x4 o = red[((wave + (z - 1) * WN * WM) * 4 * CT + t * CT + c) * 64 + lane];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[t][c][i] += o[i];
+                }
+        }
+    } else if (XT == MX4_X_F32 && a.gain) {
+        __syncthreads();
+    }
+    unsigned nan[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int mr = (wm * CT + c) * 16 + c16;
+        const int64_t m = m0 + mr;
+        if (m >= a.M) continue;
+        float rs = 1.f;
+        if constexpr (XT == MX4_X_F32)
+            if (a.gain) {
+                float ss = 0.f;
+#pragma unroll
+                for (int z = 0; z < KW * 4; ++z) ss += s_sq[z][mr];
+                rs = rms_recip(ss, a.K, a.eps);
+            }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t n = (int64_t)panel * MX4_ROWS + t * 16 + g * 4;
+            if (n >= a.N) continue;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = acc[t][c][i];
+                if (XT == MX4_X_F32 && a.gain) v[i] *= rs;
+                if (nan[t] >> i & 1u) v[i] = __uint_as_float(0x7FC00000u);
+            }
+            mx4_store(a, m, n, v);
+        }
+    }
+}
+
+// Both sides in MXFP4: the codes are the operands of the scaled 4-bit instruction as they lie in memory.  A workgroup of WN x WM
+// waves computes WN panels of w for CT WM / 4 of x, a wave one panel of w for CT 16-row tiles of x.  The tiles of x go through LDS (two
+// buffers), a wave's panel of w and all scales straight into its registers, everything two steps of 128 columns ahead: with w
+// in LDS as well its bandwidth was the bound.
+template <int CT, int WN, int WM>
+struct Mx4TileX {
+    static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_CODE_BYTES, LDS = 2 * BUF;
+    static constexpr int NT = XP * 4 / WAVES;                      // tiles of x that a wave fetches
+    static_assert(XP * 4 % WAVES == 0 && 4 % NT == 0 && CT % 4 == 0, "a wave fetches tiles of one panel");
+};
+template <int CT, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a) {
+    typedef Mx4TileX<CT, WN, WM> S;
+    extern __shared__ __attribute__((aligned(16))) char sh[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4, wn = wave % WN, wm = wave / WN;
+    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS;
+    const int n_pan = (a.N + MX4_ROWS - 1) / MX4_ROWS, m_pan = (a.M + MX4_ROWS - 1) / MX4_ROWS;
+    int tn, tm;
+    if (!mx4_tile_of((n_pan + WN - 1) / WN, (m_pan + S::XP - 1) / S::XP, tn, tm)) return;
+    struct Load { u32x4 w[4], x[S::NT]; unsigned sw, sx[CT / 4]; };
+    auto x_panel = [&](int i) { return (const char*)a.x + (size_t)min(tm * S::XP + i, m_pan - 1) * kps * MX4_PANEL_BYTES; };
+    const char* w_src = a.w + (size_t)min(tn * WN + wn, n_pan - 1) * kps * MX4_PANEL_BYTES;
+    const char* x_src = x_panel(wave * S::NT / 4) + wave * S::NT % 4 * MX4_TILE_BYTES;   // the tiles of x this wave brings to LDS
+    const char* s_src[CT / 4];                                                           // the panels of x it multiplies
+#pragma unroll
+    for (int i = 0; i < CT / 4; ++i) s_src[i] = x_panel(wm * (CT / 4) + i) + MX4_CODE_BYTES;
+    Load f0, f1;
+    unsigned bad = 0, bad_x[CT / 4];
+    f32x4 acc[4][CT];
+#pragma unroll
+    for (int i = 0; i < CT / 4; ++i) bad_x[i] = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto fetch = [&](int st, Load& f) {                            // (past the end: the last columns again, not used)
+        const size_t at = (size_t)min(st, kps - 1) * MX4_PANEL_BYTES;
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) f.x[i] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(x_src + at + i * MX4_TILE_BYTES + lane * 16));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) f.w[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(w_src + at + t * MX4_TILE_BYTES + lane * 16));
+        f.sw = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(w_src + at + MX4_CODE_BYTES + lane * 4));
+#pragma unroll
+        for (int i = 0; i < CT / 4; ++i) f.sx[i] = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(s_src[i] + at + lane * 4));
+    };
+    auto store = [&](const Load& f, char* buf) {
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) *reinterpret_cast<u32x4*>(buf + (wave * S::NT + i) * MX4_TILE_BYTES + lane * 16) = f.x[i];
+    };
+    // step st: the tiles of x lie in LDS, the rest in f, which is then free for step st + 2; next's tiles go to LDS
+    auto step = [&](int st, Load& f, const Load& next) {
+        const char* px = sh + (st & 1) * S::BUF + wm * CT * MX4_TILE_BYTES + lane * 16;
+        u32x4 w[4];
+        unsigned sx[CT / 4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = f.w[t];
+        const unsigned sw = f.sw;
+        bad |= mx4_nan_bytes(sw);
+#pragma unroll
+        for (int i = 0; i < CT / 4; ++i) { sx[i] = f.sx[i]; bad_x[i] |= mx4_nan_bytes(sx[i]); }
+        fetch(st + 2, f);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(px + c * MX4_TILE_BYTES);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t][c] = mx4_mfma(w[t], (int)(sw >> (8 * t)), x, (int)(sx[c / 4] >> (8 * (c % 4))), acc[t][c]);
+        }
+        if (st + 1 < kps) store(next, sh + (~st & 1) * S::BUF);
+        __syncthreads();
+    };
+    fetch(0, f0);
+    fetch(1, f1);
+    store(f0, sh);
+    __syncthreads();
+    for (int st = 0; st < kps; st += 2) {
+        step(st, f0, f1);
+        if (st + 1 < kps) step(st + 1, f1, f0);
+    }
+    unsigned nan[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const unsigned nan_x = mx4_nan_rows(bad_x[c / 4], c % 4) >> c16 & 1u;
+        const int64_t m = (int64_t)tm * S::XP * MX4_ROWS + (wm * CT + c) * 16 + c16;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t n = (int64_t)(tn * WN + wn) * MX4_ROWS + t * 16 + g * 4;
+            if (n >= a.N) continue;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = nan_x | (nan[t] >> i & 1u) ? __uint_as_float(0x7FC00000u) : acc[t][c][i];
+            mx4_store(a, m, n, v);
+        }
     }
 }
 

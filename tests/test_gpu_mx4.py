@@ -206,6 +206,72 @@ def test_infinities_and_nan(P, m):
     assert torch.equal(y, big[:, :2] * torch.tensor([1.0, -1.0], device="cuda"))
 
 
+# rows and outputs that take each of the kernels for many rows, with ragged last tiles in both directions
+TILES = {"float32": [(129, 11009), (300, 11009), (520, 11009)], "bfloat16": [(100, 6001), (200, 11009), (520, 11009)],
+         "mx4": [(100, 8003), (1100, 7777)]}
+
+
+@pytest.mark.parametrize("k", [20, 128, 130, 385, 512, 1000, 1281])
+@pytest.mark.parametrize("kind,m,n", [(t, *mn) for t, v in TILES.items() for mn in v])
+def test_matmul_of_many_rows(P, kind, m, n, k):
+    """Every tile kernel at reduction lengths around its steps of 128, 256 and 512 columns; float32 with and without a gain; the
+    plain products in float64 on the GPU."""
+    import torch
+    wq = P.mx4_quantize(_rows(n, k, torch.float32, k))
+    wv = P.mx4_dequantize(wq).double()
+    xf = _rows(m, k, torch.float32, k + 1)
+    if kind == "mx4":
+        x = P.mx4_quantize(xf)
+        xv = P.mx4_dequantize(x).double()
+    else:
+        x = xf.to(getattr(torch, kind))
+        xv = x.double()
+    roundings = (3 * -(-k // 32) + 16) * 2.0 ** -23
+    y = P.mx4_matmul(x, wq)
+    tol = roundings * (xv.abs() @ wv.abs().t()) + (2.0 ** -8 * (xv @ wv.t()).abs() if kind == "bfloat16" else 0.0) + 1e-37
+    assert ((y.double() - xv @ wv.t()).abs() <= tol).all()
+    assert torch.equal(y, P.mx4_matmul(x, wq))
+    if kind == "float32":
+        gain = 1.0 + 0.3 * _rows(1, k, torch.float32, 3)[0].clamp(-2, 2)
+        xh = xv * gain.double() / torch.sqrt((xv ** 2).mean(-1, keepdim=True) + 1e-5)
+        y = P.mx4_matmul(x, wq, gain=gain, eps=1e-5)
+        tol = (roundings + (k / 32 + 24) * 2.0 ** -23) * (xh.abs() @ wv.abs().t()) + 1e-37
+        assert ((y.double() - xh @ wv.t()).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("kind,m,n", [(t, *mn) for t, v in TILES.items() for mn in v])
+def test_nan_blocks_and_strides_of_many_rows(P, kind, m, n):
+    """A NaN block of w, or of x, fills its output column or row and nothing else; x's rows may lie apart and unaligned, and what
+    lies between and behind the rows of y is not touched."""
+    import torch
+    from paper_2602_05499_amd import binding as B
+    k = 700
+    wf = _rows(n, k, torch.float32, 8)
+    wf[n - 2, 699] = float("nan")
+    wf[70, 0] = float("inf")
+    wq = P.mx4_quantize(wf)
+    big = _rows(m, k + 5, torch.float32, 9)
+    if kind == "mx4":
+        big[m - 1, 300] = float("nan")
+        x = P.mx4_quantize(big[:, 3:k + 3])
+    else:
+        x = big.to(getattr(torch, kind))[:, 3:k + 3]
+    y = P.mx4_matmul(x, wq, out_dtype=torch.float32)
+    bad = torch.zeros(m, n, dtype=torch.bool, device="cuda")
+    bad[:, n - 2] = bad[:, 70] = True
+    if kind == "mx4":
+        bad[m - 1] = True
+    else:
+        assert torch.equal(P.mx4_matmul(x.contiguous(), wq, out_dtype=torch.float32).nan_to_num(), y.nan_to_num())
+    assert torch.equal(torch.isnan(y), bad) and not torch.isinf(y).any()
+    out = torch.full((m + 1, n + 3), 7.5, device="cuda")
+    code, ptr, ld = (B.SD_MX4, x.data.data_ptr(), x.data.numel()) if kind == "mx4" else \
+        ({"float32": B.SD_F32, "bfloat16": B.SD_BF16}[kind], x.data_ptr(), k + 5)
+    assert B.sd_mx4_matmul(wq.data.data_ptr(), wq.data.numel(), n, k, ptr, code, ld, m, None, 0.0, out.data_ptr(), B.SD_F32, n + 3,
+                           torch.cuda.current_stream().cuda_stream) == B.SD_OK
+    assert torch.equal(out[:m, :n].nan_to_num(), y.nan_to_num()) and (out[m:] == 7.5).all() and (out[:, n:] == 7.5).all()
+
+
 def test_rows_behind_the_result_stay_as_they_were(P):
     """ldy > N: what lies between and behind the rows of y is not touched (through the C-ABI)."""
     import torch
