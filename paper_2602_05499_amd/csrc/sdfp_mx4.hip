@@ -114,10 +114,16 @@ hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t mx4_quantize(const void* x, int x_type, int64_t ldx, int rows, int cols, void* q, hipStream_t stream) {
+template <int XT>
+static void launch_quantize(const void* x, int64_t ldx, int rows, int cols, void* q, hipStream_t s) {
     const dim3 grid((unsigned)(mx4_row_panels(rows) * mx4_col_panels(cols)));
-    if (x_type == MX4_X_F32) hipLaunchKernelGGL(k_mx4_quantize<MX4_X_F32>, grid, dim3(256), 0, stream, x, ldx, rows, cols, (char*)q);
-    else hipLaunchKernelGGL(k_mx4_quantize<MX4_X_BF16>, grid, dim3(256), 0, stream, x, ldx, rows, cols, (char*)q);
+    const bool once = (int64_t)rows * cols * (int64_t)sizeof(typename Mx4In<XT>::T) >= (int64_t)64 << 20;
+    if (once) hipLaunchKernelGGL((k_mx4_quantize<XT, true>), grid, dim3(256), 0, s, x, ldx, rows, cols, (char*)q);
+    else hipLaunchKernelGGL((k_mx4_quantize<XT, false>), grid, dim3(256), 0, s, x, ldx, rows, cols, (char*)q);
+}
+hipError_t mx4_quantize(const void* x, int x_type, int64_t ldx, int rows, int cols, void* q, hipStream_t stream) {
+    if (x_type == MX4_X_F32) launch_quantize<MX4_X_F32>(x, ldx, rows, cols, q, stream);
+    else launch_quantize<MX4_X_BF16>(x, ldx, rows, cols, q, stream);
     return hipGetLastError();
 }
 

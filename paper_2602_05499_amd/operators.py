@@ -4,6 +4,8 @@ torch and enqueues one kernel of libsdfp on the tensors' device and that device'
 raises SdError (SD_EINVAL) before anything is enqueued."""
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding as B
@@ -19,15 +21,17 @@ def _refuse(what):
     raise B.SdError(B.SD_EINVAL, what)
 
 
-def _on(index, fn, *args):
-    """fn(*args, current stream of device `index`), with the device current; a code other than SD_OK is raised."""
+def _call(name, index, *args):
+    """The entry point `name` with (*args, current stream of device `index`), with the device current; a code other than SD_OK
+    is raised."""
+    fn = getattr(B.load_library(), name)
     if torch.cuda.current_device() == index:
         rc = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
             rc = fn(*args, _raw_stream(index))
     if rc != B.SD_OK:
-        raise B.SdError(rc, fn.__name__)
+        raise B.SdError(rc, name)
 
 
 def _rows(t, where):
@@ -46,10 +50,12 @@ def _rows(t, where):
 
 def _array(t, dtypes, shape, index, where):
     """The address of a contiguous tensor of one of `dtypes` and of `shape` (None: any vector) on device `index`."""
-    if (not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.get_device() != index or not t.is_contiguous() or
-            (t.shape != shape if shape is not None else t.dim() != 1)):
-        _refuse(where)
-    return t.data_ptr()
+    try:
+        if t.dtype in dtypes and t.get_device() == index and t.is_contiguous() and (t.shape == shape if shape is not None else t.dim() == 1):
+            return t.data_ptr()
+    except AttributeError:      # no tensor at all
+        pass
+    _refuse(where)
 
 
 _I32, _I64, _F32, _BITS = (torch.int32,), (torch.int64,), (torch.float32,), (torch.int32, torch.uint32)
@@ -75,8 +81,8 @@ def mx4_quantize(x) -> Mx4:
     """Rows of float32 or bfloat16 in MXFP4 (sd_mx4_quantize)."""
     rows, cols, ld, code = _rows(x, "mx4_quantize: x")
     n = B.sd_mx4_bytes(rows, cols)
-    data = torch.empty(n, dtype=torch.uint8, device=x.device)
-    _on(x.get_device(), B.sd_mx4_quantize, x.data_ptr(), code, ld, rows, cols, data.data_ptr(), n)
+    data = x.new_empty(n, dtype=torch.uint8)
+    _call("sd_mx4_quantize", x.get_device(), x.data_ptr(), code, ld, rows, cols, data.data_ptr(), n)
     q = Mx4.__new__(Mx4)
     q.data, q.rows, q.cols = data, rows, cols
     return q
@@ -88,8 +94,8 @@ def mx4_dequantize(q: Mx4, dtype=torch.float32):
     if not isinstance(q, Mx4) or code is None:
         _refuse("mx4_dequantize: q, dtype")
     d, cols = q.data, q.cols
-    x = torch.empty((q.rows, cols), dtype=dtype, device=d.device)
-    _on(d.get_device(), B.sd_mx4_dequantize, d.data_ptr(), d.numel(), q.rows, cols, x.data_ptr(), code, cols)
+    x = d.new_empty((q.rows, cols), dtype=dtype)
+    _call("sd_mx4_dequantize", d.get_device(), d.data_ptr(), d.numel(), q.rows, cols, x.data_ptr(), code, cols)
     return x
 
 
@@ -114,8 +120,8 @@ def mx4_matmul(x, w: Mx4, gain=None, eps: float = 1e-5, out_dtype=None):
     if y_code is None or (gain is not None and code != B.SD_F32):
         _refuse("mx4_matmul: out_dtype, or a gain without float32 x")
     g = None if gain is None else _array(gain, _F32, (k,), index, "mx4_matmul: gain")
-    y = torch.empty((m, n), dtype=dtype, device=wd.device)
-    _on(index, B.sd_mx4_matmul, wd.data_ptr(), wd.numel(), n, k, xd.data_ptr(), code, ld, m, g, eps, y.data_ptr(), y_code, n)
+    y = xd.new_empty((m, n)) if dtype is xd.dtype else wd.new_empty((m, n), dtype=dtype)
+    _call("sd_mx4_matmul", index, wd.data_ptr(), wd.numel(), n, k, xd.data_ptr(), code, ld, m, g, eps, y.data_ptr(), y_code, n)
     return y
 
 
@@ -130,7 +136,7 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
     rows, vocab, ld, code = _rows(logits, "logits_rules: logits")
     index = logits.get_device()
     if out is None:
-        out, ld_out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
+        out, ld_out = torch.empty_like(logits) if ld == vocab else logits.new_empty((rows, vocab)), vocab
     else:
         r, v, ld_out, c = _rows(out, "logits_rules: out")
         if r != rows or v != vocab or c != code or out.get_device() != index:
@@ -148,6 +154,6 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
         p_allowed = _array(allowed, _BITS, (n_masks, (vocab + 31) // 32), index, "logits_rules: allowed")
         if mask_row is not None:
             m = _array(mask_row, _I32, (rows,), index, "logits_rules: mask_row")
-    _on(index, B.sd_logits_rules, logits.data_ptr(), code, ld, rows, vocab,
-        B.SdRules(repetition, presence, frequency, p_bias, p_allowed, n_masks), t, n, b, e, m, out.data_ptr(), ld_out)
+    _call("sd_logits_rules", index, logits.data_ptr(), code, ld, rows, vocab,
+        ctypes.byref(B.SdRules(repetition, presence, frequency, p_bias, p_allowed, n_masks)), t, n, b, e, m, out.data_ptr(), ld_out)
     return out
