@@ -290,7 +290,8 @@ int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_
  * of the grid 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign.  A matrix of rows x cols lies in panels of 64 rows x 128 columns,
  * [ceil(rows / 64)][ceil(cols / 128)][4352 bytes]: 4096 bytes of codes -- row 16 t + r, block b of the panel at
  * ((t * 4 + b) * 16 + r) * 16, column 2 i of the block in the low four bits of byte i, column 2 i + 1 in the high four --,
- * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes.  A scale byte 255 marks a block of NaN.
+ * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes.  A scale byte 255 marks a block of NaN
+ * (0 stands for 2^-127; what float32 cannot hold, 6 * 2^127, becomes an infinity).
  * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned. */
 size_t sd_mx4_bytes(int32_t rows, int32_t cols);
 /* Quantise rows (dtype SD_F32 or SD_BF16, ld >= cols elements apart, any alignment of their elements): the scale of a block
@@ -301,10 +302,11 @@ int sd_mx4_quantize(const void *x, int dtype, int64_t ld, int32_t rows, int32_t 
 /* The values that panels stand for, as rows of dtype SD_F32 or SD_BF16 (both exact). */
 int sd_mx4_dequantize(const void *q, size_t q_bytes, int32_t rows, int32_t cols, void *x, int dtype, int64_t ld,
                       void *hip_stream);
-/* y[M][N] = x w^T with w [N][K] in panels.  x: rows of SD_F32 (multiplied exactly, as three bfloat16 pieces) or SD_BF16, ldx
- * elements apart, or SD_MX4: panels of [M][K], ldx their size in bytes.  Sums are float32; y: rows of y_dtype SD_F32 or
+/* y[M][N] = x w^T with w [N][K] in panels.  x: rows of SD_F32 (multiplied exactly, as three bfloat16 pieces; only bits below
+ * 2^-133 are lost) or SD_BF16, ldx elements apart, or SD_MX4: panels of [M][K], ldx their size in bytes.  Sums are float32; y: rows of y_dtype SD_F32 or
  * SD_BF16, rounded once, ldy >= N elements apart.  gain: NULL, or float32 [K] with float32 x: the rows are RMS-normalised
- * first, x^ = x * gain / sqrt(mean(x^2) + eps), as in front of an output head.  The same arguments give the same bits. */
+ * first, x^ = x * gain / sqrt(mean(x^2) + eps), as in front of an output head.  y overlaps neither x nor w.  The same
+ * arguments give the same bits; a row's bits may differ with M, whose kernels add in different orders. */
 int sd_mx4_matmul(const void *w, size_t w_bytes, int32_t N, int32_t K, const void *x, int x_dtype, int64_t ldx, int32_t M,
                   const float *gain, float eps, void *y, int y_dtype, int64_t ldy, void *hip_stream);
 

@@ -1322,11 +1322,17 @@ int sd_set_rules(sd_ctx* c, const sd_rules* rules, const int32_t* next, int32_t 
     r.state = (int*)at; at += align_up(4);
     int* usable = (int*)at;
     r.usable = usable;
+    const CtxRules before = c->rules;
+    const int start_before = c->rules_start;
     c->rules = r;
     c->rules_start = rules->allowed ? state : -1;
     if (r.r.allowed) hipLaunchKernelGGL(k_rules_usable, dim3((unsigned)r.r.n_masks), dim3(256), 0, c->stream, r.r.allowed, c->cfg.vocab, usable);
     if (c->phase == PH_READY) rules_begin(c, true);
-    HIPCHK(c, hipGetLastError());
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {   // nothing was set up: the context keeps what it had
+        c->rules = before; c->rules_start = start_before;
+        HIPCHK(c, e);
+    }
     return SD_OK;
 }
 

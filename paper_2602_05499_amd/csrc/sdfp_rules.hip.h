@@ -98,7 +98,7 @@ __global__ __launch_bounds__(THREADS) void k_logits_rules(RulesRows a) {
     if (a.tokens) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(cnt + (i * THREADS + tid) * 4) = u32x4{0u, 0u, 0u, 0u};
-        const int64_t b = max(a.begin[row], (int64_t)0), e = min(a.end[row], a.n_tokens);
+        const int64_t b = min(max(a.begin[row], (int64_t)0), a.n_tokens), e = min(a.end[row], a.n_tokens);
         __syncthreads();
         auto count = [&](int tok) {
             const unsigned at = (unsigned)tok - (unsigned)lo;

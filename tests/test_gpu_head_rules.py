@@ -303,6 +303,42 @@ def test_rules_set_on_a_running_sequence_and_taken_off(P):
     raw.close()
 
 
+@pytest.mark.parametrize("vocab,K", [(1, 8), (1024, 8), (1025, 1), (300001, 8)])
+def test_picks_around_the_chunks_of_a_row(P, vocab, K):
+    """Greedy picks of draft and verify rows at vocabularies around the chunks that a row is cut into (1024 entries, longer ones
+    past 262144), at the largest depth, on rows with equal entries and with none above -inf: the lowest index of the largest."""
+    import torch
+    s = _shape("f32", vocab, K=K, d_model=64, n_heads=2, n_kv_heads=2, n_layers=2, skip_layers=(1,))
+    mask = synth.gen_skip_mask(s)
+    dw = _weights(s, mask)
+    dw.lm_head[vocab // 2:] = dw.lm_head[:vocab - vocab // 2].clone()             # every entry twice
+    torch.cuda.synchronize()
+    ses = P.Session(s, dw, mask, max_seq=64, max_k=K)
+    if vocab > 1:
+        ses.set_draft_head()
+    ses.set_rules(frequency=0.01)
+    ses.prefill(synth.gen_prompt(3, 5, vocab))
+    for _ in range(3):
+        ses.draft(K)
+        d, zq = ses.dump_draft(K), ses.dump_logits(P.SD_LOGITS_DRAFT, K)
+        ses.verify()
+        zp = ses.dump_logits(P.SD_LOGITS_VERIFY, K + 1)
+        ses.accept()
+        ses.rollback()
+        st = ses.read()[1]
+        assert [int(t) for t in d] == [int(np.argmax(r)) for r in zq]
+        n = 0
+        while n < K and d[n] == np.argmax(zp[n]):
+            n += 1
+        assert (st["last_n"], st["t_last"]) == (n, int(np.argmax(zp[n])))
+    ses.set_rules(bias=torch.full((vocab,), float("nan"), device="cuda"))
+    ses.draft(K)
+    assert (ses.dump_draft(K) == 0).all()
+    ses.verify(); ses.accept(); ses.rollback()
+    assert ses.read()[1]["last_n"] == K
+    ses.close()
+
+
 @pytest.mark.parametrize("mode", ["greedy", "sample"])
 def test_everything_together_on_another_stream(P, mode):
     """A speculative program with the MXFP4 draft head, penalties and a grammar, on a stream of its own and in a static-workspace

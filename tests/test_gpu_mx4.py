@@ -272,6 +272,45 @@ def test_nan_blocks_and_strides_of_many_rows(P, kind, m, n):
     assert torch.equal(out[:m, :n].nan_to_num(), y.nan_to_num()) and (out[m:] == 7.5).all() and (out[:, n:] == 7.5).all()
 
 
+@pytest.mark.parametrize("m", [1, 5, 16, 300])
+@pytest.mark.parametrize("e", [0, 1, 2, 127, 250])
+def test_scale_bytes_from_elsewhere(P, m, e):
+    """Panels that the caller filled: every scale byte stands for 2^(e - 127), the smallest ones too, and the codes for their
+    columns, low bits first.  Powers of two: the products are exact."""
+    import torch
+    n = 6400
+    data = torch.zeros(P.sd_mx4_bytes(n, 128), dtype=torch.uint8, device="cuda").view(n // 64, 4352)
+    data[:, 0] = 0x21                                   # row 0 of a panel: 0.5 and 1 in columns 0 and 1
+    data[:, 4096] = e
+    w = P.Mx4(data.reshape(-1), n, 128)
+    v = P.mx4_dequantize(w)
+    assert (v[0::64, 0] == 0.5 * 2.0 ** (e - 127)).all() and (v[0::64, 1] == 2.0 ** (e - 127)).all() and not v[:, 2:].any()
+    f = 2.0 ** min(100, 250 - e)
+    for col in (0, 1):
+        want = torch.zeros(m, n, device="cuda")
+        want[:, 0::64] = (0.5, 1.0)[col] * 2.0 ** (e - 127) * f
+        x = torch.zeros(m, 128, device="cuda")
+        x[:, col] = f
+        for xs in (x, x.bfloat16(), P.mx4_quantize(x)):
+            assert torch.equal(P.mx4_matmul(xs, w, out_dtype=torch.float32), want)
+
+
+def test_first_calls_inside_a_capture(P):
+    """Kernels of many rows captured, and replayed on other contents."""
+    import torch
+    w = P.mx4_quantize(_rows(11009, 300, torch.float32, 1))
+    xs = [_rows(520, 300, torch.float32, 2), _rows(520, 300, torch.bfloat16, 3), P.mx4_quantize(_rows(1100, 300, torch.float32, 4))]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ys = [P.mx4_matmul(x, w) for x in xs]
+    for seed in range(3):
+        xs[0].copy_(_rows(520, 300, torch.float32, 10 + seed))
+        xs[1].copy_(_rows(520, 300, torch.bfloat16, 20 + seed))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, P.mx4_matmul(x, w)) for x, y in zip(xs, ys))
+
+
 def test_rows_behind_the_result_stay_as_they_were(P):
     """ldy > N: what lies between and behind the rows of y is not touched (through the C-ABI)."""
     import torch

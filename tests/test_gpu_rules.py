@@ -103,6 +103,10 @@ def test_histories_empty_shared_foreign_and_out_of_range(P):
     want, mag = rules64(z.double().cpu().numpy(), tokens, begin, end, 1.25, 0.5, 0.25, None, None, None)
     _check(_run(P, z, tokens, begin, end, rep=1.25, pres=0.5, freq=0.25), want, mag, False)
     assert torch.equal(_run(P, z, tokens[:0], begin, end, rep=1.25), z)      # no tokens at all
+    far = np.full(8, 2 ** 63 - 1)                                             # ranges at the ends of 64 bits
+    assert torch.equal(_run(P, z, tokens, far, far, rep=1.25), z) and torch.equal(_run(P, z, tokens, far, -far, rep=1.25), z)
+    want, mag = rules64(z.double().cpu().numpy(), tokens, np.zeros(8, int), np.full(8, 5001), 1.25, 0.5, 0.25, None, None, None)
+    _check(_run(P, z, tokens, -far, far, rep=1.25, pres=0.5, freq=0.25), want, mag, False)
 
 
 def test_masks_per_row(P):
