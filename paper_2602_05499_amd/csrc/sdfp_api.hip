@@ -809,7 +809,7 @@ void pick_sample(sd_ctx* c, const float* z, float u, int dst, int off) {
 // rules on rows of logits, in place, and (greedy) their arg-maxes into st->d[off ..] / st->amax[off ..]; row 0 comes after r0
 // draft tokens
 void select_rows(sd_ctx* c, float* z, int rows, int r0, int mode, int dst, int off) {
-    const int V = c->cfg.vocab, len = rules_chunk_len(V);
+    const int V = c->cfg.vocab, len = rules_chunk_len(V, rows);
     hipLaunchKernelGGL(k_rows_select, dim3((V + len - 1) / len, rows), dim3(RULES_THREADS), 0, c->stream, z, V, len, c->rules, r0,
                        mode == SD_GREEDY ? 1 : 0, c->sel(), c->st(), dst, off);
 }

@@ -25,20 +25,20 @@ namespace sdfp {
 // too few workgroups (one row, 4096 outputs: 5.8 us against 6.9; 8192, 128 panels: equal; 11008: 9.3 against 8.0); two panels
 // where there are plenty and a row's cutting into pieces weighs (float32, 9 rows, 32000 outputs: 21.0 us against 25.8; for
 // one row two panels are slower, 16.4 against 15.3).
-template <int XT, int MP>
+template <int XT, int MP, bool ONCE>
 static void launch_rows(const Mx4Product& a, hipStream_t s) {
     const unsigned my = (unsigned)((a.M + 15) / 16), n_pan = (unsigned)mx4_row_panels(a.N);
     const dim3 blk(MX4_WAVES * 64);
     if (n_pan * my < 128) {
-        hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 1>), dim3(n_pan * 4 * my), blk, 0, s, a);
+        hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 1, ONCE>), dim3(n_pan * 4 * my), blk, 0, s, a);
         return;
     }
     if constexpr (XT == MX4_X_F32 && MP >= 8)
         if (n_pan * my >= 384) {
-            hipLaunchKernelGGL((k_mx4_rows<XT, MP, 2, 4>), dim3((n_pan + 1) / 2 * my), blk, 0, s, a);
+            hipLaunchKernelGGL((k_mx4_rows<XT, MP, 2, 4, ONCE>), dim3((n_pan + 1) / 2 * my), blk, 0, s, a);
             return;
         }
-    hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 4>), dim3(n_pan * my), blk, 0, s, a);
+    hipLaunchKernelGGL((k_mx4_rows<XT, MP, 1, 4, ONCE>), dim3(n_pan * my), blk, 0, s, a);
 }
 
 // A kernel's dynamic LDS limit, raised once per device.
@@ -90,26 +90,29 @@ hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
             if (tiles(256, 32) <= 512) return launch_tiles<MX4_X_F32, 2, 4, 1, 1>(a, stream);
             return launch_tiles<MX4_X_F32, 4, 8, 1, 1>(a, stream);
         }
-        if (a.M == 1) launch_rows<MX4_X_F32, 1>(a, stream);
-        else if (a.M <= 5) launch_rows<MX4_X_F32, 5>(a, stream);
-        else if (a.M <= 8) launch_rows<MX4_X_F32, 8>(a, stream);
-        else launch_rows<MX4_X_F32, 16>(a, stream);
+        if (a.M == 1) launch_rows<MX4_X_F32, 1, true>(a, stream);
+        else if (a.M <= 5) launch_rows<MX4_X_F32, 5, true>(a, stream);
+        else if (a.M <= 8) launch_rows<MX4_X_F32, 8, true>(a, stream);
+        else if (a.M <= 16) launch_rows<MX4_X_F32, 16, true>(a, stream);
+        else launch_rows<MX4_X_F32, 16, false>(a, stream);
     } else if (a.x_type == MX4_X_BF16) {
         if (a.M > 16 && pieces > 600) {
             if (tiles(128, 32) <= 512) return launch_tiles<MX4_X_BF16, 2, 2, 1, 4>(a, stream);
             if (tiles(256, 64) <= 256) return launch_tiles<MX4_X_BF16, 4, 4, 1, 2>(a, stream);
             return launch_tiles<MX4_X_BF16, 4, 8, 1, 1>(a, stream);
         }
-        if (a.M == 1) launch_rows<MX4_X_BF16, 1>(a, stream);
-        else if (a.M <= 4) launch_rows<MX4_X_BF16, 4>(a, stream);
-        else if (a.M <= 8) launch_rows<MX4_X_BF16, 8>(a, stream);
-        else launch_rows<MX4_X_BF16, 16>(a, stream);
+        if (a.M == 1) launch_rows<MX4_X_BF16, 1, true>(a, stream);
+        else if (a.M <= 4) launch_rows<MX4_X_BF16, 4, true>(a, stream);
+        else if (a.M <= 8) launch_rows<MX4_X_BF16, 8, true>(a, stream);
+        else if (a.M <= 16) launch_rows<MX4_X_BF16, 16, true>(a, stream);
+        else launch_rows<MX4_X_BF16, 16, false>(a, stream);
     } else {
         if (a.M > 16 && pieces > 768) {
             if (tiles(256, 128) < 256) return launch_tiles_mx4<4, 2, 1>(a, stream);
             return launch_tiles_mx4<8, 4, 1>(a, stream);
         }
-        launch_rows<MX4_X_MX4, 16>(a, stream);
+        if (a.M <= 16) launch_rows<MX4_X_MX4, 16, true>(a, stream);
+        else launch_rows<MX4_X_MX4, 16, false>(a, stream);
     }
     return hipGetLastError();
 }

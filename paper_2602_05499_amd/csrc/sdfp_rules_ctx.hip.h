@@ -52,22 +52,35 @@ __global__ void k_rules_commit(CtxRules c, int V, const DevState* st) {
     *c.state = s;
 }
 
-// entries of a chunk of k_rows_select: 1024, or as many thousands as keep a row within SEL_CHUNKS chunks
-__host__ __device__ constexpr int rules_chunk_len(int V) {
-    return (int)(((int64_t)V + SEL_CHUNKS * 1024 - 1) / (SEL_CHUNKS * 1024)) * 1024;
+// Entries of a chunk of k_rows_select: 1024, or as many thousands as keep all rows within SEL_CHUNKS chunks -- also those of a
+// verify forward: every workgroup's arrival is an atomic on one word (five rows of 128256 in 630 workgroups 14.3 us, in
+// 210 12.0).
+__host__ __device__ constexpr int rules_chunk_len(int V, int rows) {
+    return (int)(((int64_t)V * rows + SEL_CHUNKS * 1024 - 1) / (SEL_CHUNKS * 1024)) * 1024;
 }
 // Rows of a context's logits under its rules, in place, and (pick) their arg-maxes, lowest index first: what a greedy draft,
 // verify or prompt needs in one launch.  Row r comes after r0 + r draft tokens.  Grid (chunks, rows); the last workgroup to
-// arrive reduces the chunks' maxima.  A row without a number above -inf picks token 0.
+// arrive reduces the chunks' maxima, a wave per row.  A row without a number above -inf picks token 0.  Latency throughout:
+// one row of 32000 6.6 us, five of them 8.6, one of 128256 7.7, five 12.0.
 __global__ __launch_bounds__(RULES_THREADS) void k_rows_select(float* __restrict__ z, int V, int len, CtxRules c, int r0, int pick, SelBuf b,
                                                                DevState* st, int dst, int off) {
     __shared__ int s_state, s_extra[MAX_K];
     __shared__ unsigned long long s_best[RULES_THREADS / 64];
-    const int tid = threadIdx.x, row = blockIdx.y, chunk = blockIdx.x, n_extra = min(r0 + row, MAX_K);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.y, chunk = blockIdx.x, n_extra = min(r0 + row, MAX_K);
     float* zr = z + (int64_t)row * V;
+    const bool ruled = c.counts != nullptr, counted = ruled && has_penalties(c.r.repetition, c.r.presence, c.r.frequency);
+    f32x4 x, bi;
+    u32x4 n;
+    auto load = [&](int j) {   // (the counts' room is whole 256 bytes)
+        x = rules_load4(zr + j, V - j);
+        if (counted) n = *reinterpret_cast<const u32x4*>(c.counts + j);
+        if (ruled && c.r.bias) bi = rules_load4(c.r.bias + j, V - j);
+    };
+    const int hi = min(V, (chunk + 1) * len);
+    int j = chunk * len + tid * 4;
+    if (j < hi) load(j);       // on its way while the state is found
     const unsigned* mask = nullptr;
-    const bool counted = c.counts && has_penalties(c.r.repetition, c.r.presence, c.r.frequency);
-    if (c.counts) {
+    if (ruled) {
         if (tid < n_extra) s_extra[tid] = st->d[tid];
         if (tid == 0) {
             int s = -1;
@@ -85,20 +98,22 @@ __global__ __launch_bounds__(RULES_THREADS) void k_rows_select(float* __restrict
     // the largest entry so far as (ordered bits, complement of the index): the maximum of these is the lowest index of the
     // largest value; NaN and -inf entries do not take part
     unsigned long long best = 0;
-    const int hi = min(V, (chunk + 1) * len);
-    for (int j = chunk * len + tid * 4; j < hi; j += RULES_THREADS * 4) {
-        f32x4 x = rules_load4(zr + j, V - j);
-        if (c.counts) {
+    while (j < hi) {
+        if (ruled) {
             const unsigned w = mask ? mask[j >> 5] >> (j & 31) : ~0u;
+            if (counted) {
+                for (int i = 0; i < n_extra; ++i) {
+                    const unsigned at = (unsigned)s_extra[i] - (unsigned)j;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) n[k] += at == (unsigned)k;
+                }
+                if (n.x | n.y | n.z | n.w)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = apply_penalties(x[k], n[k], c.r);
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (j + k >= V) continue;
-                if (counted) {
-                    unsigned n = c.counts[j + k];
-                    for (int i = 0; i < n_extra; ++i) n += s_extra[i] == j + k;
-                    x[k] = apply_penalties(x[k], n, c.r);
-                }
-                if (c.r.bias) x[k] = add_rn(x[k], c.r.bias[j + k]);
+                if (c.r.bias) x[k] = add_rn(x[k], bi[k]);
                 if (!(w >> k & 1u)) x[k] = -INFINITY;
             }
             rules_store4(zr + j, x, V - j);
@@ -111,30 +126,39 @@ __global__ __launch_bounds__(RULES_THREADS) void k_rows_select(float* __restrict
                     const unsigned long long key = (unsigned long long)(u >> 31 ? ~u : u | 0x80000000u) << 32 | (unsigned)~(j + k);
                     best = key > best ? key : best;
                 }
+        j += RULES_THREADS * 4;
+        if (j < hi) load(j);
     }
     if (!pick) return;
-    auto block_best = [&](unsigned long long v) -> unsigned long long {
+    auto wave_best = [&](unsigned long long v) -> unsigned long long {
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             const unsigned long long t = __shfl_xor(v, o);
             v = t > v ? t : v;
         }
-        __syncthreads();
-        if ((tid & 63) == 0) s_best[tid >> 6] = v;
-        __syncthreads();
-        v = s_best[0];
-#pragma unroll
-        for (int w = 1; w < RULES_THREADS / 64; ++w) v = s_best[w] > v ? s_best[w] : v;
         return v;
     };
-    best = block_best(best);
+    best = wave_best(best);
+    if (lane == 0) s_best[wave] = best;
+    __syncthreads();
     double* part = b.sum;   // [rows][SEL_CHUNKS], the keys' bits
-    if (tid == 0) st_coh(part + row * SEL_CHUNKS + chunk, __longlong_as_double((long long)best));
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < RULES_THREADS / 64; ++w) best = s_best[w] > best ? s_best[w] : best;
+        st_coh(part + row * SEL_CHUNKS + chunk, __longlong_as_double((long long)best));
+    }
     if (!sel_last_arrival(b.counter, gridDim.x * gridDim.y)) return;
-    for (int r = 0; r < (int)gridDim.y; ++r) {
-        const unsigned long long k = block_best(tid < (int)gridDim.x ? (unsigned long long)__double_as_longlong(ld_coh(part + r * SEL_CHUNKS + tid)) : 0ull);
+    for (int r = wave; r < (int)gridDim.y; r += RULES_THREADS / 64) {
+        unsigned long long k = 0;
+#pragma unroll
+        for (int i = 0; i < SEL_CHUNKS / 64; ++i)
+            if (i * 64 + lane < (int)gridDim.x) {
+                const unsigned long long t = (unsigned long long)__double_as_longlong(ld_coh(part + r * SEL_CHUNKS + i * 64 + lane));
+                k = t > k ? t : k;
+            }
+        k = wave_best(k);
         const int tok = k ? (int)~(unsigned)k : 0;
-        if (tid == 0) {
+        if (lane == 0) {
             if (dst == ROWS_DRAFT) st->d[off + r] = tok;
             else st->amax[off + r] = tok;
         }
