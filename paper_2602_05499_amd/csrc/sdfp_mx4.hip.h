@@ -210,14 +210,14 @@ __device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_
     }
 }
 
-// ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head 15.4 us, 4.5 TB/s with the launch's
-// ends; 128256 x 4096 49.5 us, 5.7 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
+// ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head that lies in no cache 16.4 us, 4.2 TB/s
+// with the launch's ends; 128256 x 4096 49.4 us, 5.7 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
 // for 16 rows of x; its waves split the reduction dimension by panels and add their sums in wave order at the end.  The codes
 // go from memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies
-// the 8 values of word j), one panel ahead -- two to four ahead were slower, 17.7 to 23 us --, x through a few kilobytes of LDS
+// the 8 values of word j), one panel ahead (two: 19.5 us, their registers halve the waves in flight), x through a few kilobytes of LDS
 // that belong to the wave into the B operand, in the same order of columns.  x in MXFP4 goes as it is into the scaled 4-bit
 // instruction; float32 x is cut into three exact bfloat16 pieces, which take three of the operand's 16 columns for each row
-// while rows are few (MP <= 5: one instruction where three would run; 17.7 -> 15.5 us) and three instructions otherwise.  MP:
+// while rows are few (MP <= 5: one instruction where three would run, 17.7 -> 15.5 us) and three instructions otherwise.  MP:
 // rows of x that are staged; lanes of the operand past them read values whose results are dropped.  ONCE: one pass over the codes,
 // which then pass the caches by (codes not in any cache: 21.0 -> 19.3 us for 32000 x 5120).
 constexpr bool mx4_rows_in_columns(int xt, int mp) { return xt == MX4_X_F32 && mp <= 5; }
@@ -357,8 +357,8 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
     };
 
     const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
-    // One panel ahead.  Every load of the loop is unconditional (past the end the last panel once more): behind a load under a
-    // condition the compiler waits for everything in flight, the panel ahead included.
+    // Every load of the loop is unconditional (past the end the last panel once more): behind a load under a condition the
+    // compiler waits for everything in flight, the panel ahead included.
     Load nxt;
     if (wave < full) fetch(wave, nxt, false);
     for (int i = tid; i < NPAN * MX4_ROWS; i += W * 64) s_bad_n[i] = 0;
