@@ -12,9 +12,10 @@ from . import binding as B
 
 # A call's time on the host is its cost wherever the kernel takes a few microseconds, so the checks below use the cheapest form
 # of each question: device indexes instead of device objects, the raw handle of the current stream (torch.cuda.current_stream
-# builds an object: 2.0 us against 0.1).
+# builds an object: 2.0 us against 0.1), exceptions for what is no tensor at all.
 _CODES = {torch.float32: B.SD_F32, torch.bfloat16: B.SD_BF16}
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice       # (a tensor on a GPU exists: the runtime is up)
 
 
 def _refuse(what):
@@ -25,7 +26,7 @@ def _call(name, index, *args):
     """The entry point `name` with (*args, current stream of device `index`), with the device current; a code other than SD_OK
     is raised."""
     fn = getattr(B.load_library(), name)
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         rc = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -35,17 +36,18 @@ def _call(name, index, *args):
 
 
 def _rows(t, where):
-    """(rows, columns, distance of rows, type code) of a 2-D tensor on a GPU whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+    """(rows, columns, distance of rows, type code, device index) of a 2-D tensor on a GPU whose rows are contiguous."""
+    try:
+        n, c = t.shape
+        ld, step = t.stride()
+        code, index = _CODES[t.dtype], t.get_device()
+    except (AttributeError, ValueError, KeyError, RuntimeError, TypeError):   # no tensor, not two dimensions, another type
         _refuse(where)
-    n, c = t.shape
-    ld, step = t.stride()
-    code = _CODES.get(t.dtype)
     if n == 1:
         ld = c
-    if code is None or n < 1 or c < 1 or (step != 1 and c != 1) or ld < c:
+    if index < 0 or n < 1 or c < 1 or (step != 1 and c != 1) or ld < c:
         _refuse(where)
-    return n, c, ld, code
+    return n, c, ld, code, index
 
 
 def _array(t, dtypes, shape, index, where):
@@ -67,9 +69,12 @@ class Mx4:
     __slots__ = ("data", "rows", "cols")
 
     def __init__(self, data, rows, cols):
-        need = B.sd_mx4_bytes(rows, cols)
-        if (not isinstance(data, torch.Tensor) or not data.is_cuda or data.dtype != torch.uint8 or not data.is_contiguous() or need == 0 or
-                data.numel() < need or data.data_ptr() % 256):
+        try:
+            ok = (data.dtype is torch.uint8 and data.is_cuda and data.is_contiguous() and rows > 0 and cols > 0 and
+                  data.numel() >= (rows + 63) // 64 * ((cols + 127) // 128) * 4352 and data.data_ptr() % 256 == 0)
+        except (AttributeError, TypeError):
+            ok = False
+        if not ok:
             _refuse("Mx4: a contiguous, 256-byte aligned uint8 tensor of at least the matrix's size on a GPU")
         self.data, self.rows, self.cols = data, rows, cols
 
@@ -79,10 +84,10 @@ class Mx4:
 
 def mx4_quantize(x) -> Mx4:
     """Rows of float32 or bfloat16 in MXFP4 (sd_mx4_quantize)."""
-    rows, cols, ld, code = _rows(x, "mx4_quantize: x")
-    n = B.sd_mx4_bytes(rows, cols)
+    rows, cols, ld, code, index = _rows(x, "mx4_quantize: x")
+    n = (rows + 63) // 64 * ((cols + 127) // 128) * 4352
     data = x.new_empty(n, dtype=torch.uint8)
-    _call("sd_mx4_quantize", x.get_device(), x.data_ptr(), code, ld, rows, cols, data.data_ptr(), n)
+    _call("sd_mx4_quantize", index, x.data_ptr(), code, ld, rows, cols, data.data_ptr(), n)
     q = Mx4.__new__(Mx4)
     q.data, q.rows, q.cols = data, rows, cols
     return q
@@ -108,11 +113,11 @@ def mx4_matmul(x, w: Mx4, gain=None, eps: float = 1e-5, out_dtype=None):
     index = wd.get_device()
     if isinstance(x, Mx4):
         m, k, xd, code, dtype = x.rows, x.cols, x.data, B.SD_MX4, torch.float32
-        ld = xd.numel()
+        ld, on = xd.numel(), xd.get_device()
     else:
-        m, k, ld, code = _rows(x, "mx4_matmul: x")
+        m, k, ld, code, on = _rows(x, "mx4_matmul: x")
         xd, dtype = x, x.dtype
-    if k != w.cols or xd.get_device() != index:
+    if k != w.cols or on != index:
         _refuse("mx4_matmul: x and w of one width on one device")
     if out_dtype is not None:
         dtype = out_dtype
@@ -133,13 +138,12 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
     bias: float32 [vocab].  allowed: int32 or uint32 [n_masks][ceil(vocab / 32)], bit j % 32 of word j // 32 allows token j;
     mask_row: int32 [rows], the mask of each row (-1: none); by default row i has mask i, or all have the only one.
     out: where the result goes (`logits` itself: in place); by default a new tensor."""
-    rows, vocab, ld, code = _rows(logits, "logits_rules: logits")
-    index = logits.get_device()
+    rows, vocab, ld, code, index = _rows(logits, "logits_rules: logits")
     if out is None:
         out, ld_out = torch.empty_like(logits) if ld == vocab else logits.new_empty((rows, vocab)), vocab
     else:
-        r, v, ld_out, c = _rows(out, "logits_rules: out")
-        if r != rows or v != vocab or c != code or out.get_device() != index:
+        r, v, ld_out, c, on = _rows(out, "logits_rules: out")
+        if r != rows or v != vocab or c != code or on != index:
             _refuse("logits_rules: out")
     t = b = e = p_bias = p_allowed = m = None
     n = n_masks = 0
@@ -155,5 +159,5 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
         if mask_row is not None:
             m = _array(mask_row, _I32, (rows,), index, "logits_rules: mask_row")
     _call("sd_logits_rules", index, logits.data_ptr(), code, ld, rows, vocab,
-        ctypes.byref(B.SdRules(repetition, presence, frequency, p_bias, p_allowed, n_masks)), t, n, b, e, m, out.data_ptr(), ld_out)
+          ctypes.byref(B.SdRules(repetition, presence, frequency, p_bias, p_allowed, n_masks)), t, n, b, e, m, out.data_ptr(), ld_out)
     return out
