@@ -323,7 +323,7 @@ typedef struct {
     int32_t n_masks;             /* >= 1 where allowed is given                                             */
 } sd_rules;
 /* rows of logits z (dtype SD_F32 or SD_BF16, ld >= vocab elements apart, any alignment of their elements) to out (the same
- * type; out == z with ld_out == ld works in place, other overlaps do not).  rules: HOST.  The history of row i is
+ * type; out == z with ld_out == ld works in place, other overlaps do not and are refused where ld_out == ld).  rules: HOST.  The history of row i is
  * tokens[begin[i] .. end[i]), cut to 0 .. n_tokens: ranges may overlap, so the rows of one step can share a history; token
  * ids outside the vocabulary count for nothing, an empty range is no history.  tokens, begin and end are read only if some
  * penalty is set.  mask_row[i]: the mask of row i, a value outside 0 .. n_masks - 1 leaves the row unmasked; NULL: mask i,

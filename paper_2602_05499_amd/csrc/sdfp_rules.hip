@@ -30,6 +30,11 @@ extern "C" int sd_logits_rules(const void* z, int dtype, int64_t ld, int32_t row
     if (((uintptr_t)z | (uintptr_t)out) & (es - 1)) return SD_EINVAL;
     if (!rules_ok(*rules)) return SD_EINVAL;
     if (z == out && ld != ld_out) return SD_EINVAL;     // in place: the same rows
+    if (z != out && ld == ld_out) {                     // rows of out across rows of z
+        const uintptr_t d = ((uintptr_t)z > (uintptr_t)out ? (uintptr_t)z - (uintptr_t)out : (uintptr_t)out - (uintptr_t)z) / es;
+        const uint64_t n = d / (uint64_t)ld, q = d % (uint64_t)ld;
+        if ((q < (uint64_t)vocab && n < (uint64_t)rows) || ((uint64_t)ld - q < (uint64_t)vocab && n + 1 < (uint64_t)rows)) return SD_EINVAL;
+    }
     RulesRows a = {};
     a.z = z; a.out = out; a.ld = ld; a.ld_out = ld_out; a.rows = rows; a.vocab = vocab;
     a.r = rule_set(*rules);

@@ -1,7 +1,7 @@
 """The operators of the output head's way to a token, on torch tensors: MXFP4 matrices (`mx4_quantize`, `mx4_dequantize`,
 `mx4_matmul`) and rules on logits (`logits_rules`).  Marshalling only: each call checks its tensors, allocates its result with
 torch and enqueues one kernel of libsdfp on the tensors' device and that device's current stream.  What the checks refuse
-raises SdError (SD_EINVAL) before anything is enqueued."""
+raises SdError (SD_EINVAL) before anything is enqueued.  Nothing is recorded for a gradient."""
 from __future__ import annotations
 
 import ctypes
@@ -16,6 +16,7 @@ from . import binding as B
 _CODES = {torch.float32: B.SD_F32, torch.bfloat16: B.SD_BF16}
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice       # (a tensor on a GPU exists: the runtime is up)
+_END = 1 << 31                                    # sizes are 32-bit at the entry points, and ctypes would cut larger ones
 
 
 def _refuse(what):
@@ -45,7 +46,7 @@ def _rows(t, where):
         _refuse(where)
     if n == 1:
         ld = c
-    if index < 0 or n < 1 or c < 1 or (step != 1 and c != 1) or ld < c:
+    if index < 0 or not 0 < n < _END or not 0 < c < _END or (step != 1 and c != 1) or ld < c:
         _refuse(where)
     return n, c, ld, code, index
 
@@ -70,7 +71,7 @@ class Mx4:
 
     def __init__(self, data, rows, cols):
         try:
-            ok = (data.dtype is torch.uint8 and data.is_cuda and data.is_contiguous() and rows > 0 and cols > 0 and
+            ok = (data.dtype is torch.uint8 and data.is_cuda and data.is_contiguous() and 0 < rows < _END and 0 < cols < _END and
                   data.numel() >= (rows + 63) // 64 * ((cols + 127) // 128) * 4352 and data.data_ptr() % 256 == 0)
         except (AttributeError, TypeError):
             ok = False
@@ -155,6 +156,8 @@ def logits_rules(logits, tokens=None, begin=None, end=None, *, repetition: float
         p_bias = _array(bias, _F32, (vocab,), index, "logits_rules: bias")
     if allowed is not None:
         n_masks = allowed.shape[0] if isinstance(allowed, torch.Tensor) and allowed.dim() else 0
+        if not 0 < n_masks < _END:
+            _refuse("logits_rules: allowed")
         p_allowed = _array(allowed, _BITS, (n_masks, (vocab + 31) // 32), index, "logits_rules: allowed")
         if mask_row is not None:
             m = _array(mask_row, _I32, (rows,), index, "logits_rules: mask_row")

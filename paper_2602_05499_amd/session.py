@@ -240,7 +240,7 @@ class Session:
 
     def set_draft_head(self, head=True):
         """The draft's output head in MXFP4 (sd_set_draft_head): an Mx4 of [vocab][d_model], True to quantise the model's
-        lm_head, False or None to go back to lm_head."""
+        lm_head, False or None to go back to lm_head.  An Mx4 may still be in the making on the current stream."""
         if head is None or head is False:
             self._check(B.sd_set_draft_head(self.ctx, None, 0), "sd_set_draft_head")
             self.sync()
@@ -253,14 +253,22 @@ class Session:
         s = self.shape
         if not isinstance(head, Mx4) or (head.rows, head.cols) != (s.vocab, s.d_model) or head.data.device != self.kv.device:
             raise B.SdError(B.SD_EINVAL, "set_draft_head")
+        self._after_current()
         self._check(B.sd_set_draft_head(self.ctx, head.data.data_ptr(), head.data.numel()), "sd_set_draft_head")
         self._retired.append(self.draft_head)
         self.draft_head = head
 
+    def _after_current(self):
+        """The context's stream goes on after what the current stream holds so far."""
+        now = self.torch.cuda.current_stream(self.kv.device)
+        if now != self.stream:
+            self.stream.wait_stream(now)
+
     def set_rules(self, *, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, next=None, state=0):
         """Rules on every row of logits before a token is picked from it (sd_set_rules).  bias: float32 [vocab]; allowed:
         int32 or uint32 [n_masks][ceil(vocab / 32)]; next: int32 [n_masks][vocab], the grammar's state behind each token;
-        state: the start.  Called without arguments: no rules."""
+        state: the start.  The tensors may still be in the making on the current stream.  Called without arguments: no
+        rules."""
         torch, s, dev = self.torch, self.shape, self.kv.device
         if repetition == 1.0 and presence == 0.0 and frequency == 0.0 and bias is None and allowed is None and next is None:
             self._check(B.sd_set_rules(self.ctx, None, None, 0, None, 0), "sd_set_rules")
@@ -275,13 +283,18 @@ class Session:
                 raise B.SdError(B.SD_EINVAL, "set_rules")
             return t.data_ptr()
 
-        n = 0 if allowed is None else allowed.shape[0]
+        n = 0
+        if allowed is not None:
+            n = allowed.shape[0] if isinstance(allowed, torch.Tensor) and allowed.dim() else 0
+            if n < 1 or not -1 <= state < n:
+                raise B.SdError(B.SD_EINVAL, "set_rules")
         r = B.SdRules(repetition, presence, frequency, ptr(bias, (torch.float32,), (s.vocab,)),
                       ptr(allowed, (torch.int32, torch.uint32), (n, (s.vocab + 31) // 32)), n)
         nx = ptr(next, (torch.int32,), (n, s.vocab))
         need = B.sd_rules_bytes(self.cfg, n)
         with torch.cuda.stream(self.stream):
             buf = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._after_current()
         self._check(B.sd_set_rules(self.ctx, r, nx, state, buf.data_ptr(), need), "sd_set_rules")
         self._retired.append(self.rules)
         self.rules = (buf, bias, allowed, next)

@@ -303,6 +303,45 @@ def test_rules_set_on_a_running_sequence_and_taken_off(P):
     raw.close()
 
 
+def test_tensors_still_in_the_making(P):
+    """A head and rules whose tensors the current stream has yet to write, for a context on another stream; refused arguments
+    leave what was set."""
+    import torch
+    s = _shape("bf16", 2050)
+    mask = synth.gen_skip_mask(s)
+    dw = _weights(s, mask)
+    prompt = synth.gen_prompt(3, 21, s.vocab)
+    dev, _ = _rule_sets(s.vocab, np.random.default_rng(5))["all"]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    ses = P.Session(s, dw, mask, max_seq=128, max_k=4, stream=stream)
+    ses.set_draft_head(P.mx4_quantize(dw.lm_head))
+    ses.set_rules(**dev)
+    want, stats = ses.generate(prompt, 24, 4)
+    torch.cuda.synchronize()
+    big = torch.randn(4096, 4096, device="cuda")
+    late = {k: torch.zeros_like(v) if isinstance(v, torch.Tensor) else v for k, v in dev.items()}
+    head = P.Mx4(torch.zeros_like(ses.draft_head.data), s.vocab, s.d_model)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big = (big @ big).clamp_(-1, 1)                      # what the writes below wait behind
+    head.data.copy_(ses.draft_head.data)
+    for k, v in late.items():
+        if isinstance(v, torch.Tensor):
+            v.copy_(dev[k])
+    ses.set_draft_head(head)
+    ses.set_rules(**late)
+    got, again = ses.generate(prompt, 24, 4)
+    assert np.array_equal(got, want) and again["accepted"] == stats["accepted"]
+    one = dev["allowed"][:1]
+    for bad in (dict(allowed=one[:0]), dict(allowed=5), dict(allowed=one, state=1), dict(allowed=one, state=2 ** 32), dict(allowed=one, state=-2)):
+        with pytest.raises(P.SdError) as e:
+            ses.set_rules(**bad)
+        assert e.value.code == P.SD_EINVAL
+    assert np.array_equal(ses.generate(prompt, 24, 4)[0], want)
+    ses.close()
+
+
 @pytest.mark.parametrize("vocab,K", [(1, 8), (1024, 8), (1025, 1), (300001, 8)])
 def test_picks_around_the_chunks_of_a_row(P, vocab, K):
     """Greedy picks of draft and verify rows at vocabularies around the chunks that a row is cut into (1024 entries, longer ones

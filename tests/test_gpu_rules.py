@@ -178,6 +178,34 @@ def test_refusals(P):
         assert e.value.code == P.SD_EINVAL
 
 
+def test_rows_between_rows_and_refused_overlaps(P):
+    """z and out may lie between one another's rows, never across them; no masks at all is no rule but a mistake."""
+    import torch
+    buf = torch.randn(3, 260, device="cuda", generator=torch.Generator("cuda").manual_seed(8))
+    z, before = buf[:, :100], buf.clone()
+    bias = torch.linspace(-2, 2, 100, device="cuda")
+    for at in (100, 130, 160):
+        out = P.logits_rules(z, bias=bias, out=buf[:, at:at + 100])
+        assert torch.equal(out, before[:, :100] + bias) and torch.equal(z, before[:, :100])
+    flat = buf.view(-1)
+    for bad in (dict(out=buf[:, 1:101]), dict(out=flat[200:720].view(2, 260)[:, :100]), dict(allowed=torch.zeros(0, 4, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(P.SdError) as e:
+            P.logits_rules(z[:bad["out"].shape[0]] if "out" in bad else z, **bad)
+        assert e.value.code == P.SD_EINVAL
+
+
+def test_more_rows_than_an_int_are_refused(P):
+    """Sizes are 32-bit: 2^32 + 5 rows must not be taken for 5."""
+    import torch
+    z = torch.empty(2 ** 32 + 5, 1, dtype=torch.bfloat16, device="cuda")
+    w = P.mx4_quantize(torch.ones(1, 1, device="cuda"))
+    for call in (lambda: P.logits_rules(z, out=z), lambda: P.mx4_quantize(z), lambda: P.mx4_matmul(z, w), lambda: P.mx4_quantize(z.view(1, -1)),
+                 lambda: P.Mx4(w.data, 2 ** 32 + 1, 1)):
+        with pytest.raises(P.SdError) as e:
+            call()
+        assert e.value.code == P.SD_EINVAL
+
+
 def test_other_stream_and_captured_graph(P):
     import torch
     z, tokens, begin, end, bias, allowed = _case(4, 5000, "float32", 9)

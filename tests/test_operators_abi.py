@@ -86,6 +86,16 @@ def test_logits_rules_refuse(over, rules):
     assert B.sd_logits_rules(A, B.SD_F32, 100, 3, 100, None, A, 10, A, A, None, A + 4096, 100, None) == B.SD_EINVAL
 
 
+@pytest.mark.parametrize("dtype,es", [(B.SD_F32, 4), (B.SD_BF16, 2)])
+@pytest.mark.parametrize("off", [1, 99, 229, 231, 290, 619, -1, -99, -161, -520])
+def test_rows_across_rows_are_refused(dtype, es, off):
+    """out as rows of 100 at distance 260, moved by off elements against z: each of these shares entries with z's three rows."""
+    mine = {r * 260 + i for r in range(3) for i in range(100)}
+    assert mine & {off + e for e in mine}
+    z = A + (1 << 20)
+    assert B.sd_logits_rules(z, dtype, 260, 3, 100, _rules(), None, 0, None, None, None, z + off * es, 260, None) == B.SD_EINVAL
+
+
 def test_tensors_that_are_no_gpu_rows_are_refused():
     import torch
     import paper_2602_05499_amd as P
