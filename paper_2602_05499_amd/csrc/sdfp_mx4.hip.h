@@ -210,6 +210,49 @@ __device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_
     }
 }
 
+// What a wave of the kernels for many rows has computed for 16 rows of x, m0 .. m0 + 15, and 64 outputs, n0 .. n0 + 63: lane 16 g + r
+// holds in v[t] the outputs 16 t + 4 g .. of row r.  It goes through 4352 bytes of LDS of the wave's own, so that each store
+// writes whole lines of 128 bytes; a result beyond what the caches hold passes them by (x in MXFP4, 4096 rows x 14336 x 4096,
+// float32 result: 127 us, stored from the lanes as they are 159; bfloat16 result 125 and 164).
+constexpr int MX4_OUT_BYTES = 16 * 68 * 4;
+__device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, int64_t m0, int64_t n0, const f32x4 (&v)[4]) {
+    const int lane = threadIdx.x & 63, es = a.y_type == MX4_X_F32 ? 4 : 2;
+    float* sh = reinterpret_cast<float*>(lds);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(sh + (lane & 15) * 68 + t * 16 + (lane >> 4) * 4) = v[t];
+    __builtin_amdgcn_wave_barrier();
+    const bool once = (int64_t)a.M * a.N * es >= (int64_t)64 << 20;
+    if (a.y_type == MX4_X_F32) {
+        const int64_t n = n0 + lane % 16 * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 4 + lane / 16;
+            const u32x4 o = *reinterpret_cast<const u32x4*>(sh + r * 68 + lane % 16 * 4);
+            float* y = (float*)a.y + (m0 + r) * a.ldy + n;
+            if (m0 + r >= a.M || n >= a.N) continue;
+            if (n + 4 > a.N)
+                for (int e = 0; n + e < a.N; ++e) y[e] = __uint_as_float(o[e]);
+            else if (once) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(y));
+            else *reinterpret_cast<u32x4_any*>(y) = o;
+        }
+    } else {
+        const int64_t n = n0 + lane % 8 * 8;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = i * 8 + lane / 8;
+            const f32x4 p = *reinterpret_cast<const f32x4*>(sh + r * 68 + lane % 8 * 8), q = *reinterpret_cast<const f32x4*>(sh + r * 68 + lane % 8 * 8 + 4);
+            const u32x4 o{pack_bf16(p.x, p.y), pack_bf16(p.z, p.w), pack_bf16(q.x, q.y), pack_bf16(q.z, q.w)};
+            bf16_t* y = (bf16_t*)a.y + (m0 + r) * a.ldy + n;
+            if (m0 + r >= a.M || n >= a.N) continue;
+            if (n + 8 > a.N)
+                for (int e = 0; n + e < a.N; ++e) y[e] = (bf16_t)(o[e / 2] >> (16 * (e % 2)));
+            else if (once) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(y));
+            else *reinterpret_cast<u32x4_any*>(y) = o;
+        }
+    }
+}
+
 // ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head that lies in no cache 16.4 us, 4.2 TB/s
 // with the launch's ends; 128256 x 4096 49.4 us, 5.7 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
 // for 16 rows of x; its waves split the reduction dimension by panels and add their sums in wave order at the end.  The codes
@@ -436,7 +479,7 @@ struct Mx4Tile {
     static constexpr int THREADS = 64 * WN * WM * KW, TM = 16 * CT * WM, NPC = XT == MX4_X_F32 ? 3 : 1;
     static constexpr int PANEL = NPC * TM * 256, BUF = KW * PANEL; // bytes of x: 128 columns, a step
     static constexpr int RED = (KW - 1) * WN * WM * 64 * 16 * CT * 4;
-    static constexpr int LDS = 2 * BUF > RED ? 2 * BUF : RED;
+    static constexpr int LDS = 2 * BUF > RED + WN * WM * MX4_OUT_BYTES ? 2 * BUF : RED + WN * WM * MX4_OUT_BYTES;
     static constexpr int WAVES = WN * WM * KW;
     static constexpr int PER_K = TM / 4 / WAVES, NCH = KW * PER_K; // 8-element pieces of x that a thread stages: of 128 columns, in all
     static constexpr int AHEAD = NPC == 3 ? 2 : 4;                 // units whose operands are read ahead
@@ -490,11 +533,13 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 #pragma unroll
     for (int i = 0; i < S::PER_K; ++i) xrow[i] = (const T*)a.x + min(m0 + (tile0 + i * (S::WAVES / 4)) * 16 + c16, (int64_t)a.M - 1) * a.ldx;
     const float* gain = a.gain ? a.gain : (const float*)a.x;       // (without a gain: loaded, not used)
-    auto fetch = [&](int st, Load& f, bool full) {
+    auto fetch_codes = [&](int st, Load& f) {
         const char* p = wp + (size_t)min(st * KW + kg, kps - 1) * MX4_PANEL_BYTES;
 #pragma unroll
         for (int t = 0; t < 4; ++t) f.code[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(p + t * MX4_TILE_BYTES + lane * 16));
         f.scale = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(p + MX4_CODE_BYTES + lane * 4));
+    };
+    auto fetch_x = [&](int st, Load& f, bool full) {
 #pragma unroll
         for (int z = 0; z < KW; ++z) {
             const int64_t k = (int64_t)(st * KW + z) * MX4_COLS + blk * 32 + g * 8;
@@ -506,7 +551,7 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
             }
         }
     };
-    auto store_x = [&](const Load& f, char* buf) {
+    auto store_x = [&](const Load& f, char* buf, bool count) {   // count: their squares belong to the rows' sums
 #pragma unroll
         for (int i = 0; i < S::NCH; ++i) {
             char* to = buf + i / S::PER_K * S::PANEL + ((tile0 + i % S::PER_K * (S::WAVES / 4)) * 4 + g) * 1024 + (blk * 16 + c16) * 16;
@@ -517,8 +562,10 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
                 if (a.gain) {
                     Mx4In<XT>::unpack(f.gain[i / S::PER_K][0], *reinterpret_cast<float(*)[4]>(gn));
                     Mx4In<XT>::unpack(f.gain[i / S::PER_K][1], *reinterpret_cast<float(*)[4]>(gn + 4));
+                    float ss = sq[i];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { sq[i] = fmaf(v[e], v[e], sq[i]); v[e] *= gn[e]; }
+                    for (int e = 0; e < 8; ++e) { ss = fmaf(v[e], v[e], ss); v[e] *= gn[e]; }
+                    sq[i] = count ? ss : sq[i];
                 }
                 unsigned pk[3][4];
                 trunc3(v, pk);
@@ -529,13 +576,14 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
             }
         }
     };
-    auto multiply = [&](const char* buf, const u32x4 (&code)[4], unsigned scale) {
+    // decoded: called when the codes in f are not needed any more
+    auto multiply = [&](const char* buf, Load& f, auto decoded) {
         buf += kg * S::PANEL + wm * CT * 4096 + lane * 16;
-        bad |= mx4_nan_bytes(scale);
+        bad |= mx4_nan_bytes(f.scale);
         float s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const unsigned e = scale >> (8 * t) & 255u;
+            const unsigned e = f.scale >> (8 * t) & 255u;
             s[t] = __uint_as_float(e == 0u ? 0x00400000u : e << 23);
         }
         // unit u: sub-step u / CT, row tile u % CT; its operands are read S::AHEAD units earlier, and while a sub-step's units
@@ -549,7 +597,7 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 #pragma unroll
         for (int u = 0; u < S::AHEAD; ++u) read(u);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) wb[0][t] = mx4_decode(code[t][0], s[t]);
+        for (int t = 0; t < 4; ++t) wb[0][t] = mx4_decode(f.code[t][0], s[t]);
 #pragma unroll
         for (int u = 0; u < 4 * CT; ++u) {
             const int j = u / CT, c = u % CT;
@@ -560,8 +608,9 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
             if (u + S::AHEAD < 4 * CT) read(u + S::AHEAD);
             if (j < 3)
 #pragma unroll
-                for (int t = 4 * c / CT; t < 4 * (c + 1) / CT; ++t) wb[~j & 1][t] = mx4_decode(code[t][j + 1], s[t]);
+                for (int t = 4 * c / CT; t < 4 * (c + 1) / CT; ++t) wb[~j & 1][t] = mx4_decode(f.code[t][j + 1], s[t]);
             __builtin_amdgcn_sched_barrier(0);
+            if (u == 3 * CT - 1) decoded();
         }
     };
     // Step st: x lies in LDS, the codes in f, which is then free for step st + 2; next, on its way since the step before, goes to LDS.
@@ -569,19 +618,17 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
     // compiler waits for everything in flight.
     const int full = a.K / (MX4_COLS * KW);                        // steps without a ragged end
     auto step = [&](int st, Load& f, const Load& next) {
-        u32x4 code[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) code[t] = f.code[t];
-        const unsigned scale = f.scale;
-        fetch(min(st + 2, full - 1), f, true);
-        multiply(sh + (st & 1) * S::BUF, code, scale);
-        if (st + 1 < full) store_x(next, sh + (~st & 1) * S::BUF);
+        const int then = min(st + 2, full - 1);
+        fetch_x(then, f, true);
+        multiply(sh + (st & 1) * S::BUF, f, [&] { fetch_codes(then, f); });
+        store_x(next, sh + (~st & 1) * S::BUF, st + 1 < full);
         __syncthreads();
     };
+    auto fetch = [&](int st, Load& f, bool full) { fetch_codes(st, f); fetch_x(st, f, full); };
     if (full > 0) {
         fetch(0, f0, true);
         fetch(min(1, full - 1), f1, true);
-        store_x(f0, sh);
+        store_x(f0, sh, true);
         __syncthreads();
         int st = 0;
         for (; st + 1 < full; st += 2) { step(st, f0, f1); step(st + 1, f1, f0); }
@@ -589,9 +636,9 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
     }
     if (full < steps) {
         fetch(full, f0, false);
-        store_x(f0, sh);
+        store_x(f0, sh, true);
         __syncthreads();
-        if (full * KW + kg < kps) multiply(sh, f0.code, f0.scale);
+        if (full * KW + kg < kps) multiply(sh, f0, [] {});
         __syncthreads();
     }
     if constexpr (XT == MX4_X_F32)
@@ -635,30 +682,25 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
     for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int mr = (wm * CT + c) * 16 + c16;
-        const int64_t m = m0 + mr;
-        if (m >= a.M) continue;
+        const int mr = (wm * CT + c) * 16;
         float rs = 1.f;
         if constexpr (XT == MX4_X_F32)
             if (a.gain) {
                 float ss = 0.f;
 #pragma unroll
-                for (int z = 0; z < KW * 4; ++z) ss += s_sq[z][mr];
+                for (int z = 0; z < KW * 4; ++z) ss += s_sq[z][mr + c16];
                 rs = rms_recip(ss, a.K, a.eps);
             }
+        f32x4 v[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t n = (int64_t)panel * MX4_ROWS + t * 16 + g * 4;
-            if (n >= a.N) continue;
-            float v[4];
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[i] = acc[t][c][i];
-                if (XT == MX4_X_F32 && a.gain) v[i] *= rs;
-                if (nan[t] >> i & 1u) v[i] = __uint_as_float(0x7FC00000u);
+                v[t][i] = acc[t][c][i];
+                if (XT == MX4_X_F32 && a.gain) v[t][i] *= rs;
+                if (nan[t] >> i & 1u) v[t][i] = __uint_as_float(0x7FC00000u);
             }
-            mx4_store(a, m, n, v);
-        }
+        mx4_store_tile(a, sh + S::RED + wave * MX4_OUT_BYTES, m0 + mr, (int64_t)panel * MX4_ROWS, v);
     }
 }
 
@@ -668,9 +710,11 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 // in LDS as well its bandwidth was the bound.
 template <int CT, int WN, int WM>
 struct Mx4TileX {
-    static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_CODE_BYTES, LDS = 2 * BUF;
+    static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_PANEL_BYTES;   // all tiles of x, then their scales
+    static constexpr int LDS = 2 * BUF > WAVES * MX4_OUT_BYTES ? 2 * BUF : WAVES * MX4_OUT_BYTES;
     static constexpr int NT = XP * 4 / WAVES;                      // tiles of x that a wave fetches
-    static_assert(XP * 4 % WAVES == 0 && 4 % NT == 0 && CT % 4 == 0, "a wave fetches tiles of one panel");
+    static constexpr int NS = XP * 64 / WAVES;                     // words of scales of x
+    static_assert(XP * 4 % WAVES == 0 && 4 % NT == 0 && CT % 4 == 0 && 64 % NS == 0, "a wave fetches parts of one panel");
 };
 template <int CT, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a) {
@@ -681,13 +725,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
     const int n_pan = (a.N + MX4_ROWS - 1) / MX4_ROWS, m_pan = (a.M + MX4_ROWS - 1) / MX4_ROWS;
     int tn, tm;
     if (!mx4_tile_of((n_pan + WN - 1) / WN, (m_pan + S::XP - 1) / S::XP, tn, tm)) return;
-    struct Load { u32x4 w[4], x[S::NT]; unsigned sw, sx[CT / 4]; };
+    struct Load { u32x4 w[4], x[S::NT]; unsigned sw, sx; };
     auto x_panel = [&](int i) { return (const char*)a.x + (size_t)min(tm * S::XP + i, m_pan - 1) * kps * MX4_PANEL_BYTES; };
     const char* w_src = a.w + (size_t)min(tn * WN + wn, n_pan - 1) * kps * MX4_PANEL_BYTES;
     const char* x_src = x_panel(wave * S::NT / 4) + wave * S::NT % 4 * MX4_TILE_BYTES;   // the tiles of x this wave brings to LDS
-    const char* s_src[CT / 4];                                                           // the panels of x it multiplies
-#pragma unroll
-    for (int i = 0; i < CT / 4; ++i) s_src[i] = x_panel(wm * (CT / 4) + i) + MX4_CODE_BYTES;
+    const int s_at = wave * S::NS + lane % S::NS;                                        // and the word of their scales
+    const char* s_src = x_panel(s_at / 64) + MX4_CODE_BYTES + s_at % 64 * 4;
     Load f0, f1;
     unsigned bad = 0, bad_x[CT / 4];
     f32x4 acc[4][CT];
@@ -697,66 +740,75 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto fetch = [&](int st, Load& f) {                            // (past the end: the last columns again, not used)
-        const size_t at = (size_t)min(st, kps - 1) * MX4_PANEL_BYTES;
+    // loads of a step (past the end: the last columns again, not used), each into registers that the step two before has done
+    // with: loads that wait in registers of their own end in copies, and a copy waits for its load
+    auto at = [&](int st) { return (size_t)min(st, kps - 1) * MX4_PANEL_BYTES; };
+    auto fetch_x = [&](int st, Load& f) {
 #pragma unroll
-        for (int i = 0; i < S::NT; ++i) f.x[i] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(x_src + at + i * MX4_TILE_BYTES + lane * 16));
-#pragma unroll
-        for (int t = 0; t < 4; ++t) f.w[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(w_src + at + t * MX4_TILE_BYTES + lane * 16));
-        f.sw = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(w_src + at + MX4_CODE_BYTES + lane * 4));
-#pragma unroll
-        for (int i = 0; i < CT / 4; ++i) f.sx[i] = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(s_src[i] + at + lane * 4));
+        for (int i = 0; i < S::NT; ++i) f.x[i] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(x_src + at(st) + i * MX4_TILE_BYTES + lane * 16));
+        f.sx = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(s_src + at(st)));
+    };
+    auto fetch_w = [&](int st, int t, Load& f) {
+        f.w[t] = *reinterpret_cast<const SDFP_GLOBAL u32x4*>(as_global(w_src + at(st) + t * MX4_TILE_BYTES + lane * 16));
+    };
+    auto fetch_s = [&](int st, Load& f) {
+        f.sw = *reinterpret_cast<const SDFP_GLOBAL unsigned*>(as_global(w_src + at(st) + MX4_CODE_BYTES + lane * 4));
     };
     auto store = [&](const Load& f, char* buf) {
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) *reinterpret_cast<u32x4*>(buf + (wave * S::NT + i) * MX4_TILE_BYTES + lane * 16) = f.x[i];
+        *reinterpret_cast<unsigned*>(buf + S::XP * MX4_CODE_BYTES + s_at * 4) = f.sx;
     };
-    // step st: the tiles of x lie in LDS, the rest in f, which is then free for step st + 2; next's tiles go to LDS
+    // step st: the tiles of x lie in LDS, the rest in f; next's tiles go to LDS
     auto step = [&](int st, Load& f, const Load& next) {
         const char* px = sh + (st & 1) * S::BUF + wm * CT * MX4_TILE_BYTES + lane * 16;
-        u32x4 w[4];
+        const char* ps = sh + (st & 1) * S::BUF + S::XP * MX4_CODE_BYTES + wm * CT * 64 + lane * 4;
         unsigned sx[CT / 4];
+        u32x4 x[CT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) w[t] = f.w[t];
-        const unsigned sw = f.sw;
-        bad |= mx4_nan_bytes(sw);
+        for (int i = 0; i < CT / 4; ++i) sx[i] = *reinterpret_cast<const unsigned*>(ps + i * 256);
 #pragma unroll
-        for (int i = 0; i < CT / 4; ++i) { sx[i] = f.sx[i]; bad_x[i] |= mx4_nan_bytes(sx[i]); }
-        fetch(st + 2, f);
+        for (int c = 0; c < CT; ++c) x[c] = *reinterpret_cast<const u32x4*>(px + c * MX4_TILE_BYTES);
+        fetch_x(st + 2, f);
+        bad |= mx4_nan_bytes(f.sw);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(px + c * MX4_TILE_BYTES);
+        for (int i = 0; i < CT / 4; ++i) bad_x[i] |= mx4_nan_bytes(sx[i]);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t][c] = mx4_mfma(w[t], (int)(sw >> (8 * t)), x, (int)(sx[c / 4] >> (8 * (c % 4))), acc[t][c]);
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[t][c] = mx4_mfma(f.w[t], (int)(f.sw >> (8 * t)), x[c], (int)(sx[c / 4] >> (8 * (c % 4))), acc[t][c]);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_w(st + 2, t, f);
         }
-        if (st + 1 < kps) store(next, sh + (~st & 1) * S::BUF);
+        fetch_s(st + 2, f);
+        store(next, sh + (~st & 1) * S::BUF);
         __syncthreads();
+    };
+    auto fetch = [&](int st, Load& f) {
+        fetch_x(st, f);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) fetch_w(st, t, f);
+        fetch_s(st, f);
     };
     fetch(0, f0);
     fetch(1, f1);
     store(f0, sh);
     __syncthreads();
-    for (int st = 0; st < kps; st += 2) {
-        step(st, f0, f1);
-        if (st + 1 < kps) step(st + 1, f1, f0);
-    }
+    int st = 0;
+    for (; st + 1 < kps; st += 2) { step(st, f0, f1); step(st + 1, f1, f0); }
+    if (st < kps) step(st, f0, f1);
     unsigned nan[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const unsigned nan_x = mx4_nan_rows(bad_x[c / 4], c % 4) >> c16 & 1u;
-        const int64_t m = (int64_t)tm * S::XP * MX4_ROWS + (wm * CT + c) * 16 + c16;
-        if (m >= a.M) continue;
+        f32x4 v[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t n = (int64_t)(tn * WN + wn) * MX4_ROWS + t * 16 + g * 4;
-            if (n >= a.N) continue;
-            float v[4];
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = nan_x | (nan[t] >> i & 1u) ? __uint_as_float(0x7FC00000u) : acc[t][c][i];
-            mx4_store(a, m, n, v);
-        }
+            for (int i = 0; i < 4; ++i) v[t][i] = nan_x | (nan[t] >> i & 1u) ? __uint_as_float(0x7FC00000u) : acc[t][c][i];
+        mx4_store_tile(a, sh + wave * MX4_OUT_BYTES, (int64_t)tm * S::XP * MX4_ROWS + (wm * CT + c) * 16, (int64_t)(tn * WN + wn) * MX4_ROWS, v);
     }
 }
 

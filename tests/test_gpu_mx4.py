@@ -272,6 +272,30 @@ def test_nan_blocks_and_strides_of_many_rows(P, kind, m, n):
     assert torch.equal(out[:m, :n].nan_to_num(), y.nan_to_num()) and (out[m:] == 7.5).all() and (out[:, n:] == 7.5).all()
 
 
+@pytest.mark.parametrize("m,n", [(4200, 8195), (1040, 1037)])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "mx4"])
+def test_results_of_both_types_within_wider_rows(P, kind, m, n):
+    """Results larger and smaller than the caches in both types, as rows at an odd distance, ending inside a panel: the values, and
+    nothing beside them."""
+    import torch
+    from paper_2602_05499_amd import binding as B
+    k = 130
+    wq = P.mx4_quantize(_rows(n, k, torch.float32, 8))
+    xf = _rows(m, k, torch.float32, 9)
+    x = P.mx4_quantize(xf) if kind == "mx4" else xf.to(getattr(torch, kind))
+    xv, wv = (P.mx4_dequantize(x) if kind == "mx4" else x).double(), P.mx4_dequantize(wq).double()
+    want, mag = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    code, ptr, ld = (B.SD_MX4, x.data.data_ptr(), x.data.numel()) if kind == "mx4" else \
+        ({"float32": B.SD_F32, "bfloat16": B.SD_BF16}[kind], x.data_ptr(), k)
+    for out, y_code, step in ((torch.float32, B.SD_F32, 0.0), (torch.bfloat16, B.SD_BF16, 2.0 ** -8)):
+        y = torch.full((m + 1, n + 6), 7.5, dtype=out, device="cuda")
+        assert B.sd_mx4_matmul(wq.data.data_ptr(), wq.data.numel(), n, k, ptr, code, ld, m, None, 0.0, y[:, 3:].data_ptr(), y_code, n + 6,
+                               torch.cuda.current_stream().cuda_stream) == B.SD_OK
+        tol = (3 * -(-k // 32) + 16) * 2.0 ** -23 * mag + step * want.abs() + 1e-37
+        assert ((y[:m, 3:n + 3].double() - want).abs() <= tol).all()
+        assert (y[m:] == 7.5).all() and (y[:, :3] == 7.5).all() and (y[:, n + 3:] == 7.5).all()
+
+
 @pytest.mark.parametrize("m", [1, 5, 16, 300])
 @pytest.mark.parametrize("e", [0, 1, 2, 127, 250])
 def test_scale_bytes_from_elsewhere(P, m, e):
