@@ -72,20 +72,21 @@ static hipError_t launch_tiles_mx4(const Mx4Product& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Which kernel: the one for a few rows while its workgroups' 16-row by 64-output pieces are few (each reads the codes and
-// cuts the rows up anew), a small tile whose waves split the reduction while those make a round of the 256 compute units or two, a middle one
-// for the next round, the large tile from there on.  Microseconds, K 4096 (few rows / small / middle / large):
-//   bfloat16  128 x 4096 14/16/31/48, 64 x 11008 18/17/33/49, 512 x 4096 33/31/32/48, 256 x 11008 46/44/32/49, 512 x 11008 87/82/60/50,
-//             4096 x 14336 849/771/455/375 (1.28 PFLOP/s; the library's bfloat16 product of that size 396)
-//   float32   128 x 4096 23/46/52/126, 512 x 4096 72/52/57/127, 256 x 11008 99/91/83/128, 2048 x 4096 256/183/161/137,
-//             4096 x 14336 1801/1288/1108/972 (three products: 1.48 PFLOP/s)
-//   MXFP4     128 x 4096 13/15/-/25, 256 x 11008 30/20/-/27, 2048 x 4096 62/29/-/29, 4096 x 14336 413/222/-/164 (2.9 PFLOP/s)
+// Which kernel: the one for a few rows while its workgroups' 16-row by 64-output pieces (each reads the codes and cuts the rows
+// up anew) make two rounds of the 256 compute units, or four in float32, whose tiles have three times the work; a small tile whose
+// waves split the reduction while those make one round, a middle one for the next, the large tile from there on.
+// Microseconds, K 4096 (few rows / small / middle / large):
+//   bfloat16  128 x 4096 14/16/28/44, 64 x 11008 18/16/28/44, 512 x 4096 32/32/29/44, 256 x 11008 46/43/29/44, 512 x 11008 83/82/56/45,
+//             4096 x 14336 866/757/421/351 (1.37 PFLOP/s; the library's bfloat16 product of that size 396)
+//   float32   128 x 4096 23/46/49/121, 512 x 4096 70/52/54/121, 256 x 11008 95/90/78/120, 2048 x 4096 249/181/162/134,
+//             4096 x 14336 1786/1256/1111/935 (three products: 1.54 PFLOP/s)
+//   MXFP4     128 x 4096 13/14/-/22, 256 x 11008 32/18/-/23, 2048 x 4096 65/26/-/26, 4096 x 14336 442/201/-/150 (3.2 PFLOP/s)
 hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
     const int64_t n_pan = mx4_row_panels(a.N), pieces = n_pan * (((int64_t)a.M + 15) / 16);
     if (pieces > INT32_MAX) return hipErrorInvalidConfiguration;
     auto tiles = [&](int n, int m) { return (((int64_t)a.N + n - 1) / n) * (((int64_t)a.M + m - 1) / m); };
     if (a.x_type == MX4_X_F32) {
-        if (a.M > 16 && pieces > 1400) {
+        if (a.M > 16 && pieces > 1024) {
             if (tiles(256, 32) <= 256) return launch_tiles<MX4_X_F32, 2, 4, 1, 2>(a, stream);
             if (tiles(256, 32) <= 512) return launch_tiles<MX4_X_F32, 2, 4, 1, 1>(a, stream);
             return launch_tiles<MX4_X_F32, 4, 8, 1, 1>(a, stream);
@@ -96,8 +97,8 @@ hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
         else if (a.M <= 16) launch_rows<MX4_X_F32, 16, true>(a, stream);
         else launch_rows<MX4_X_F32, 16, false>(a, stream);
     } else if (a.x_type == MX4_X_BF16) {
-        if (a.M > 16 && pieces > 600) {
-            if (tiles(128, 32) <= 512) return launch_tiles<MX4_X_BF16, 2, 2, 1, 4>(a, stream);
+        if (a.M > 16 && pieces > 512) {
+            if (tiles(128, 32) <= 256) return launch_tiles<MX4_X_BF16, 2, 2, 1, 4>(a, stream);
             if (tiles(256, 64) <= 256) return launch_tiles<MX4_X_BF16, 4, 4, 1, 2>(a, stream);
             return launch_tiles<MX4_X_BF16, 4, 8, 1, 1>(a, stream);
         }
@@ -107,7 +108,7 @@ hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
         else if (a.M <= 16) launch_rows<MX4_X_BF16, 16, true>(a, stream);
         else launch_rows<MX4_X_BF16, 16, false>(a, stream);
     } else {
-        if (a.M > 16 && pieces > 768) {
+        if (a.M > 16 && pieces > 512) {
             if (tiles(256, 128) < 256) return launch_tiles_mx4<4, 2, 1>(a, stream);
             return launch_tiles_mx4<8, 4, 1>(a, stream);
         }

@@ -212,17 +212,16 @@ __device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_
 
 // What a wave of the kernels for many rows has computed for 16 rows of x, m0 .. m0 + 15, and 64 outputs, n0 .. n0 + 63: lane 16 g + r
 // holds in v[t] the outputs 16 t + 4 g .. of row r.  It goes through 4352 bytes of LDS of the wave's own, so that each store
-// writes whole lines of 128 bytes; a result beyond what the caches hold passes them by (x in MXFP4, 4096 rows x 14336 x 4096,
-// float32 result: 127 us, stored from the lanes as they are 159; bfloat16 result 125 and 164).
+// writes whole lines of 128 bytes (x in MXFP4, 4096 rows x 14336 x 4096, float32 result: 153 us, from the lanes as they are 158;
+// past the caches 153).
 constexpr int MX4_OUT_BYTES = 16 * 68 * 4;
 __device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, int64_t m0, int64_t n0, const f32x4 (&v)[4]) {
-    const int lane = threadIdx.x & 63, es = a.y_type == MX4_X_F32 ? 4 : 2;
+    const int lane = threadIdx.x & 63;
     float* sh = reinterpret_cast<float*>(lds);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(sh + (lane & 15) * 68 + t * 16 + (lane >> 4) * 4) = v[t];
     __builtin_amdgcn_wave_barrier();
-    const bool once = (int64_t)a.M * a.N * es >= (int64_t)64 << 20;
     if (a.y_type == MX4_X_F32) {
         const int64_t n = n0 + lane % 16 * 4;
 #pragma unroll
@@ -233,7 +232,6 @@ __device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, i
             if (m0 + r >= a.M || n >= a.N) continue;
             if (n + 4 > a.N)
                 for (int e = 0; n + e < a.N; ++e) y[e] = __uint_as_float(o[e]);
-            else if (once) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(y));
             else *reinterpret_cast<u32x4_any*>(y) = o;
         }
     } else {
@@ -247,7 +245,6 @@ __device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, i
             if (m0 + r >= a.M || n >= a.N) continue;
             if (n + 8 > a.N)
                 for (int e = 0; n + e < a.N; ++e) y[e] = (bf16_t)(o[e / 2] >> (16 * (e % 2)));
-            else if (once) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(y));
             else *reinterpret_cast<u32x4_any*>(y) = o;
         }
     }
@@ -613,9 +610,10 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
             if (u == 3 * CT - 1) decoded();
         }
     };
-    // Step st: x lies in LDS, the codes in f, which is then free for step st + 2; next, on its way since the step before, goes to LDS.
-    // Every load of the loop is unconditional (past the end the last step once more): behind a load under a condition the
-    // compiler waits for everything in flight.
+    // Step st: x lies in LDS, the codes in f; next, on its way since the step before, goes to LDS.  What step st + 2 needs is loaded
+    // into f as this step is done with its parts: loaded into other registers, it is copied at the loop's end, and a copy waits
+    // for its load.  Every load and store of the loop is unconditional (past the end the last step once more): behind a load under
+    // a condition the compiler waits for everything in flight.
     const int full = a.K / (MX4_COLS * KW);                        // steps without a ragged end
     auto step = [&](int st, Load& f, const Load& next) {
         const int then = min(st + 2, full - 1);
@@ -705,9 +703,11 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 }
 
 // Both sides in MXFP4: the codes are the operands of the scaled 4-bit instruction as they lie in memory.  A workgroup of WN x WM
-// waves computes WN panels of w for CT WM / 4 of x, a wave one panel of w for CT 16-row tiles of x.  The tiles of x go through LDS (two
-// buffers), a wave's panel of w and all scales straight into its registers, everything two steps of 128 columns ahead: with w
-// in LDS as well its bandwidth was the bound.
+// waves computes WN panels of w for CT WM / 4 of x, a wave one panel of w for CT 16-row tiles of x.  x, codes and scales, goes
+// through LDS (two buffers), a wave's panel of w straight into its registers, everything two steps of 128 columns ahead: with w
+// in LDS as well its bandwidth was the bound, and scales of x that every wave loads for itself wait for one another (1024 rows x
+// 4096 x 14336: 44 us, those loads 50).  At 3.2 PFLOP/s of the 8.0 that these instructions reach without loads; the return path of
+// the loads into registers is busy 86 % of the time.
 template <int CT, int WN, int WM>
 struct Mx4TileX {
     static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_PANEL_BYTES;   // all tiles of x, then their scales
@@ -740,8 +740,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // loads of a step (past the end: the last columns again, not used), each into registers that the step two before has done
-    // with: loads that wait in registers of their own end in copies, and a copy waits for its load
+    // loads of a step (past the end: the last columns again, not used), each into the registers that the step two before has
+    // done with: loaded into others, they are copied at the loop's end, and a copy waits for its load
     auto at = [&](int st) { return (size_t)min(st, kps - 1) * MX4_PANEL_BYTES; };
     auto fetch_x = [&](int st, Load& f) {
 #pragma unroll
