@@ -706,8 +706,9 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 // waves computes WN panels of w for CT WM / 4 of x, a wave one panel of w for CT 16-row tiles of x.  x, codes and scales, goes
 // through LDS (two buffers), a wave's panel of w straight into its registers, everything two steps of 128 columns ahead: with w
 // in LDS as well its bandwidth was the bound, and scales of x that every wave loads for itself wait for one another (1024 rows x
-// 4096 x 14336: 44 us, those loads 50).  At 3.2 PFLOP/s of the 8.0 that these instructions reach without loads; the return path of
-// the loads into registers is busy 86 % of the time.
+// 4096 x 14336: 44 us, those loads 50).  4096 rows x 14336 x 4096 at 3.2 PFLOP/s, 4096 x 4096 x 14336 at 4.3, of the 8.0 that these
+// instructions reach without loads; of the former's 150 us 42 are the write of 235 MB of float32 results, which nothing hides
+// (workgroups started at different times: the same).
 template <int CT, int WN, int WM>
 struct Mx4TileX {
     static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_PANEL_BYTES;   // all tiles of x, then their scales
