@@ -392,3 +392,27 @@ def test_other_stream_and_captured_graph(P, m):
         torch.cuda.synchronize()
         eager = P.mx4_matmul(P.mx4_quantize(P.mx4_matmul(xin, w, gain=gain)), P.mx4_quantize(wf[:, :200]))
         assert torch.equal(out, eager)
+
+
+def test_offsets_past_32_bits(P):
+    """Two million rows of 4097: more than 2^32 elements and bytes of panels; the last rows as the same rows on their own."""
+    import torch
+    head, cols = 2 ** 21, 4097
+    x = torch.zeros(head + 70, cols, dtype=torch.bfloat16, device="cuda")
+    tail = _rows(70, cols, torch.bfloat16, 4)
+    x[head:] = tail
+    q, qt = P.mx4_quantize(x), P.mx4_quantize(tail)
+    assert q.data.numel() > 2 ** 32 and torch.equal(q.data[-qt.data.numel():], qt.data)
+    few = _rows(3, cols, torch.float32, 5)
+    wt = P.mx4_dequantize(qt).double()
+    tol = (3 * -(-cols // 32) + 16) * 2.0 ** -23 * (few.double().abs() @ wt.abs().t()) + 1e-37
+    y = P.mx4_matmul(few, q)
+    assert ((y[:, head:].double() - few.double() @ wt.t()).abs() <= tol).all() and not y[:, :head].any()
+    small = P.mx4_quantize(_rows(64, cols, torch.float32, 6))
+    ws = P.mx4_dequantize(small).double()
+    for many, tv in ((x, tail.double()), (q, wt)):
+        y = P.mx4_matmul(many, small, out_dtype=torch.float32)
+        tol = (3 * -(-cols // 32) + 16) * 2.0 ** -23 * (tv.abs() @ ws.abs().t()) + 1e-37
+        assert ((y[head:].double() - tv @ ws.t()).abs() <= tol).all() and not y[:head].any()
+    back = P.mx4_dequantize(q, torch.bfloat16)
+    assert torch.equal(back[head:], P.mx4_dequantize(qt, torch.bfloat16)) and not back[:64].any()

@@ -227,3 +227,22 @@ def test_other_stream_and_captured_graph(P):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, P.logits_rules(z, *dev, **kw))
+
+
+def test_offsets_past_32_bits(P):
+    """9 GB of logits in place: the last rows, four billion entries in, as the same rows on their own."""
+    import torch
+    rows, vocab = 70000, 65537
+    z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    z[-3:] = torch.randn(3, vocab, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).bfloat16()
+    bias = torch.linspace(-3, 3, vocab, device="cuda")
+    allowed = torch.full((1, -(-vocab // 32)), 0x5A5A5A5A, dtype=torch.int32, device="cuda")
+    tokens = torch.arange(0, vocab, 7, dtype=torch.int32, device="cuda")
+    begin = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    kw = dict(repetition=1.25, presence=0.5, bias=bias, allowed=allowed)
+    end = torch.zeros_like(begin)
+    end[-2:] = tokens.numel()
+    want = P.logits_rules(z[-3:].clone(), tokens, begin[-3:], end[-3:].clone(), **kw)
+    first = P.logits_rules(z[:1].clone(), tokens, begin[:1], end[:1], **kw)
+    assert P.logits_rules(z, tokens, begin, end, out=z, **kw) is z
+    assert torch.equal(z[-3:], want) and torch.equal(z[:1], first) and torch.equal(z[rows // 2:rows // 2 + 1], first)
