@@ -292,7 +292,8 @@ int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_
  * ((t * 4 + b) * 16 + r) * 16, column 2 i of the block in the low four bits of byte i, column 2 i + 1 in the high four --,
  * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes.  A scale byte 255 marks a block of NaN
  * (0 stands for 2^-127; what float32 cannot hold, 6 * 2^127, becomes an infinity).
- * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned. */
+ * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned.  A matrix that is
+ * quantised, read back or multiplied has fewer than 2^24 panels. */
 size_t sd_mx4_bytes(int32_t rows, int32_t cols);
 /* Quantise rows (dtype SD_F32 or SD_BF16, ld >= cols elements apart, any alignment of their elements): the scale of a block
  * is 2^(floor(log2 max|x|) - 2), at least 2^-126, and every value is rounded to the nearest grid value (ties to the even

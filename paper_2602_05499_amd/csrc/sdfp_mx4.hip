@@ -11,8 +11,9 @@ static_assert(SD_F32 == MX4_X_F32 && SD_BF16 == MX4_X_BF16 && SD_MX4 == MX4_X_MX
 namespace {
 bool row_type(int t) { return t == SD_F32 || t == SD_BF16; }
 bool size_ok(int rows, int cols) { return rows >= 1 && cols >= 1 && rows <= INT32_MAX - 1024 && cols <= INT32_MAX - 1024; }   // (sizes are rounded up in int)
-// panels of a matrix, as the grid of a launch: SD_EINVAL past what a launch can hold
-bool grid_ok(int rows, int cols) { return (int64_t)mx4_row_panels(rows) * mx4_col_panels(cols) <= INT32_MAX; }
+// workgroups of a launch, which holds 2^32 - 1 threads; a matrix's panels by 256 threads each
+bool launch_ok(int64_t groups, int threads) { return groups <= UINT32_MAX / threads; }
+bool grid_ok(int rows, int cols) { return launch_ok((int64_t)mx4_row_panels(rows) * mx4_col_panels(cols), 256); }
 bool rows_ok(const void* x, int type, int64_t ld, int cols) {
     return x && row_type(type) && ld >= cols && ((uintptr_t)x & (type == SD_F32 ? 3 : 1)) == 0;
 }
@@ -83,7 +84,6 @@ static hipError_t launch_tiles_mx4(const Mx4Product& a, hipStream_t s) {
 //   MXFP4     128 x 4096 13/14/-/22, 256 x 11008 32/18/-/23, 2048 x 4096 65/26/-/26, 4096 x 14336 442/201/-/150 (3.2 PFLOP/s)
 hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
     const int64_t n_pan = mx4_row_panels(a.N), pieces = n_pan * (((int64_t)a.M + 15) / 16);
-    if (pieces > INT32_MAX) return hipErrorInvalidConfiguration;
     auto tiles = [&](int n, int m) { return (((int64_t)a.N + n - 1) / n) * (((int64_t)a.M + m - 1) / m); };
     if (a.x_type == MX4_X_F32) {
         if (a.M > 16 && pieces > 1024) {
@@ -159,7 +159,7 @@ int sd_mx4_matmul(const void* w, size_t w_bytes, int32_t N, int32_t K, const voi
     if (x_dtype == SD_MX4 ? !x || ((uintptr_t)x & 255) || ldx < 0 || !grid_ok(M, K) : !rows_ok(x, x_dtype, ldx, K)) return SD_EINVAL;
     if (gain && (x_dtype != SD_F32 || ((uintptr_t)gain & 3) || !(eps >= 0.f))) return SD_EINVAL;
     if (w_bytes < mx4_bytes(N, K) || (x_dtype == SD_MX4 && (size_t)ldx < mx4_bytes(M, K))) return SD_ENOMEM;
-    if ((int64_t)mx4_row_panels(N) * (((int64_t)M + 15) / 16) > INT32_MAX) return SD_EINVAL;
+    if (!launch_ok(M <= 16 ? mx4_row_panels(N) : (((int64_t)N + 255) / 256) * (((int64_t)M + 63) / 64), 512)) return SD_EINVAL;
     const Mx4Product a{(const char*)w, x, gain, y, ldx, ldy, M, N, K, x_dtype, y_dtype, eps};
     return status(mx4_product(a, (hipStream_t)hip_stream));
 }

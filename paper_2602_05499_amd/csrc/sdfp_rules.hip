@@ -10,13 +10,24 @@ namespace {
 // entries 4.0 to 6.0; five of 128256 4.6 against 5.2 to 6.8).  Once 4096-entry chunks of 256 threads still make four
 // workgroups per compute unit, those: a row's history is read half as often (256 rows of 32003 in bfloat16 13.4 us against
 // 16.7, 64 of 128256 13.8 against 16.4 -- 4.9 TB/s, a large copy 4.7).
+// A launch holds 2^32 - 1 threads: beyond those (millions of rows) several follow each other.
+template <typename T, int THREADS, int NV>
+hipError_t launch_rows(RulesRows a, int rows, hipStream_t s) {
+    constexpr int CH = THREADS * 4 * NV;
+    const int chunks = (a.vocab + CH - 1) / CH, most = (int)(UINT32_MAX / THREADS) / chunks;
+    for (int64_t r = 0; r < rows; r += most) {
+        a.row0 = (int)r;
+        const unsigned n = (unsigned)(rows - r < most ? rows - r : most) * (unsigned)chunks;
+        hipLaunchKernelGGL((k_logits_rules<T, THREADS, NV>), dim3(n), dim3(THREADS), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 template <typename T>
-hipError_t launch(const RulesRows& a, hipStream_t s) {
-    auto chunks = [&](int ch) { return (int64_t)a.rows * ((a.vocab + ch - 1) / ch); };
-    if (chunks(2048) > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (chunks(4096) >= 1024) hipLaunchKernelGGL((k_logits_rules<T, 256, 4>), dim3((unsigned)chunks(4096)), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_logits_rules<T, 512, 1>), dim3((unsigned)chunks(2048)), dim3(512), 0, s, a);
-    return hipGetLastError();
+hipError_t launch(const RulesRows& a, int rows, hipStream_t s) {
+    if ((int64_t)rows * ((a.vocab + 4095) / 4096) >= 1024) return launch_rows<T, 256, 4>(a, rows, s);
+    return launch_rows<T, 512, 1>(a, rows, s);
 }
 
 }  // namespace
@@ -36,7 +47,7 @@ extern "C" int sd_logits_rules(const void* z, int dtype, int64_t ld, int32_t row
         if ((q < (uint64_t)vocab && n < (uint64_t)rows) || ((uint64_t)ld - q < (uint64_t)vocab && n + 1 < (uint64_t)rows)) return SD_EINVAL;
     }
     RulesRows a = {};
-    a.z = z; a.out = out; a.ld = ld; a.ld_out = ld_out; a.rows = rows; a.vocab = vocab;
+    a.z = z; a.out = out; a.ld = ld; a.ld_out = ld_out; a.vocab = vocab;
     a.r = rule_set(*rules);
     if (has_penalties(a.r.repetition, a.r.presence, a.r.frequency)) {
         if (n_tokens < 0 || (n_tokens > 0 && !tokens) || !begin || !end) return SD_EINVAL;
@@ -49,5 +60,5 @@ extern "C" int sd_logits_rules(const void* z, int dtype, int64_t ld, int32_t row
         a.mask_row = mask_row;
     }
     hipStream_t s = (hipStream_t)hip_stream;
-    return (dtype == SD_F32 ? launch<float>(a, s) : launch<bf16_t>(a, s)) == hipSuccess ? SD_OK : SD_EHIP;
+    return (dtype == SD_F32 ? launch<float>(a, rows, s) : launch<bf16_t>(a, rows, s)) == hipSuccess ? SD_OK : SD_EHIP;
 }

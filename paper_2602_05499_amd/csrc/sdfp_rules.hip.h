@@ -65,7 +65,7 @@ constexpr int RULES_THREADS = 256;
 struct RulesRows {
     const void* z; void* out;
     int64_t ld, ld_out;
-    int rows, vocab;
+    int row0, vocab;              // the launch's first row
     RuleSet r;
     const int* tokens;            // [n_tokens], or nullptr: no penalties
     int64_t n_tokens;
@@ -76,8 +76,8 @@ template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void k_logits_rules(RulesRows a) {
     constexpr int CH = THREADS * 4 * NV;
     __shared__ __attribute__((aligned(16))) unsigned cnt[CH];
-    const int tid = threadIdx.x, chunks = (a.vocab + CH - 1) / CH, row = blockIdx.x / chunks;
-    const int lo = (blockIdx.x - row * chunks) * CH;
+    const int tid = threadIdx.x, chunks = (a.vocab + CH - 1) / CH, in = blockIdx.x / chunks, row = a.row0 + in;
+    const int lo = (blockIdx.x - in * chunks) * CH;
     const T* z = reinterpret_cast<const T*>(a.z) + (int64_t)row * a.ld + lo;
     const int have = a.vocab - lo;
     const unsigned* mask = nullptr;

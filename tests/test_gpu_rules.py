@@ -246,3 +246,20 @@ def test_offsets_past_32_bits(P):
     first = P.logits_rules(z[:1].clone(), tokens, begin[:1], end[:1], **kw)
     assert P.logits_rules(z, tokens, begin, end, out=z, **kw) is z
     assert torch.equal(z[-3:], want) and torch.equal(z[:1], first) and torch.equal(z[rows // 2:rows // 2 + 1], first)
+
+
+@pytest.mark.parametrize("rows,vocab", [(2 ** 24 + 77, 3), (2 ** 23 + 5, 4097)])
+def test_more_rows_than_a_launch_holds(P, rows, vocab):
+    """16777215 workgroups of 256 threads are a launch; rows past them, masks by row and histories among them, come in the next."""
+    import torch
+    z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    i = torch.arange(rows, device="cuda")
+    z[:, 0] = (i % 251).bfloat16()
+    tokens = torch.tensor([0, 0, 1], dtype=torch.int32, device="cuda")
+    end = torch.where(i % 3 == 0, 3, 0)
+    allowed = torch.tensor([[-1], [-3]], dtype=torch.int32, device="cuda").expand(2, -(-vocab // 32)).contiguous()
+    got = P.logits_rules(z, tokens, torch.zeros_like(i), end, frequency=0.5, presence=1.0, allowed=allowed,
+                         mask_row=(i % 2).int(), out=z)
+    hit = (i % 3 == 0).float()
+    first, second = (i % 251).float() - 2.0 * hit, torch.where(i % 2 == 1, -float("inf"), -1.5 * hit)
+    assert torch.equal(got[:, 0], first.bfloat16()) and torch.equal(got[:, 1], second.bfloat16()) and not got[:, 2].any()

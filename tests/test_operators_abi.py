@@ -86,6 +86,17 @@ def test_logits_rules_refuse(over, rules):
     assert B.sd_logits_rules(A, B.SD_F32, 100, 3, 100, None, A, 10, A, A, None, A + 4096, 100, None) == B.SD_EINVAL
 
 
+def test_more_than_a_launch_holds_is_refused():
+    """2^32 - 1 threads: 256 per panel of a matrix, 512 per panel of outputs of a product with few rows."""
+    rows = 64 * 2 ** 24
+    n = B.sd_mx4_bytes(rows, 1)
+    assert n == 2 ** 24 * 4352
+    assert B.sd_mx4_quantize(A, B.SD_F32, 1, rows, 1, A, n, None) == B.SD_EINVAL
+    assert B.sd_mx4_dequantize(A, n, rows, 1, A, B.SD_F32, 1, None) == B.SD_EINVAL
+    for M, N in ((1, rows), (3, rows // 2), (16, rows // 2), (2 ** 30, 64), (2 ** 28, 1025)):
+        assert B.sd_mx4_matmul(A, B.sd_mx4_bytes(N, 1), N, 1, A, B.SD_BF16, 1, M, None, 0.0, A, B.SD_F32, N, None) == B.SD_EINVAL
+
+
 @pytest.mark.parametrize("dtype,es", [(B.SD_F32, 4), (B.SD_BF16, 2)])
 @pytest.mark.parametrize("off", [1, 99, 229, 231, 290, 619, -1, -99, -161, -520])
 def test_rows_across_rows_are_refused(dtype, es, off):
