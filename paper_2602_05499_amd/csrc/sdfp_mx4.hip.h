@@ -250,11 +250,11 @@ __device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, i
     }
 }
 
-// ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head that lies in no cache 16.4 us, 4.2 TB/s
-// with the launch's ends; 128256 x 4096 49.4 us, 5.7 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
+// ---- product of a few rows: bound by the read of the panels (one row of a 32000 x 4096 head that lies in no cache 15.3 us, 4.6 TB/s
+// with the launch's ends; 128256 x 4096 46.5 us, 6.0 TB/s; x in MXFP4 5 rows 43.3 us, 6.5 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
 // for 16 rows of x; its waves split the reduction dimension by panels and add their sums in wave order at the end.  The codes
 // go from memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies
-// the 8 values of word j), one panel ahead (two: 19.5 us, their registers halve the waves in flight), x through a few kilobytes of LDS
+// the 8 values of word j), one panel ahead, x through a few kilobytes of LDS
 // that belong to the wave into the B operand, in the same order of columns.  x in MXFP4 goes as it is into the scaled 4-bit
 // instruction; float32 x is cut into three exact bfloat16 pieces, which take three of the operand's 16 columns for each row
 // while rows are few (MP <= 5: one instruction where three would run, 17.7 -> 15.5 us) and three instructions otherwise.  MP:
@@ -397,18 +397,38 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
     };
 
     const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
-    // Every load of the loop is unconditional (past the end the last panel once more): behind a load under a condition the
+    // Every load of the loops is unconditional (past the end the last panel once more): behind a load under a condition the
     // compiler waits for everything in flight, the panel ahead included.
     Load nxt;
     if (wave < full) fetch(wave, nxt, false);
     for (int i = tid; i < NPAN * MX4_ROWS; i += W * 64) s_bad_n[i] = 0;
     if (tid < 16) s_bad_m[tid] = 0;
-    for (int kp = wave; kp < full; kp += W) {
-        const Load cur = nxt;
-        fetch(min(kp + W, full - 1), nxt, false);
-        multiply(cur);
+    if constexpr (XT == MX4_X_MX4) {
+        // two panels ahead, each loaded into the registers that are done with (one row of 32000 x 4096 13.1 us, one panel ahead
+        // 13.8; the other kinds' longer steps gain nothing from it: five float32 rows 19.8 against 17.6)
+        Load aft;
+        int kp = wave;
+        if (kp + W < full) fetch(kp + W, aft, false);
+        for (; kp + 3 * W < full; kp += 2 * W) {
+            multiply(nxt);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(kp + 2 * W, nxt, false);
+            multiply(aft);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(kp + 3 * W, aft, false);
+        }
+        if (kp < full) multiply(nxt);
+        if (kp + 2 * W < full) fetch(kp + 2 * W, nxt, false);
+        if (kp + W < full) multiply(aft);
+        if (kp + 2 * W < full) multiply(nxt);
+    } else {
+        for (int kp = wave; kp < full; kp += W) {
+            const Load cur = nxt;
+            fetch(min(kp + W, full - 1), nxt, false);
+            multiply(cur);
+        }
+        if (full < kps && full % W == wave) { fetch(full, nxt, true); multiply(nxt); }
     }
-    if (full < kps && full % W == wave) { fetch(full, nxt, true); multiply(nxt); }
 
     // the waves' sums, in wave order (and the pieces' after one another), a panel at a time
     __syncthreads();
