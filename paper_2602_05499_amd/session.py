@@ -164,6 +164,12 @@ class Session:
         if rc != B.SD_OK:
             raise B.SdError(rc, where, B.sd_last_hip_error(self.ctx) if getattr(self, "ctx", None) else 0)
 
+    def _waited(self, rc, where):
+        """_check for the calls that always wait for the stream (sd_set_skip_mask and sd_dump_logits need not): nothing that was
+        enqueued while a replaced tensor was in use runs any more."""
+        self._check(rc, where)
+        self._retired.clear()
+
     def close(self):
         if getattr(self, "ctx", None):
             B.sd_free(self.ctx)
@@ -184,7 +190,7 @@ class Session:
         self._check(B.sd_set_skip_mask(self.ctx, np.ascontiguousarray(mask, np.uint8)), "sd_set_skip_mask")
 
     def prefill(self, prompt, mode=B.SD_GREEDY, u=None):
-        self._check(B.sd_prefill(self.ctx, np.ascontiguousarray(prompt, np.int32), mode, self._u(u)), "sd_prefill")
+        self._waited(B.sd_prefill(self.ctx, np.ascontiguousarray(prompt, np.int32), mode, self._u(u)), "sd_prefill")
 
     def draft(self, K, mode=B.SD_GREEDY, u=None):
         self._check(B.sd_draft(self.ctx, K, mode, self._u(u)), "sd_draft")
@@ -255,7 +261,8 @@ class Session:
             raise B.SdError(B.SD_EINVAL, "set_draft_head")
         self._after_current()
         self._check(B.sd_set_draft_head(self.ctx, head.data.data_ptr(), head.data.numel()), "sd_set_draft_head")
-        self._retired.append(self.draft_head)
+        if self.draft_head is not None:
+            self._retired.append(self.draft_head)
         self.draft_head = head
 
     def _after_current(self):
@@ -296,7 +303,8 @@ class Session:
             buf = torch.empty(need, dtype=torch.uint8, device=dev)
         self._after_current()
         self._check(B.sd_set_rules(self.ctx, r, nx, state, buf.data_ptr(), need), "sd_set_rules")
-        self._retired.append(self.rules)
+        if self.rules is not None:
+            self._retired.append(self.rules)
         self.rules = (buf, bias, allowed, next)
 
     def phase_trace(self, on=True):
@@ -306,7 +314,7 @@ class Session:
         """[(tag, microseconds since the first entry)] of the most recent forward's workgroup 0."""
         buf = np.zeros(1024, np.uint64)
         n = ctypes.c_int32(0)
-        self._check(B.sd_phase_trace_read(self.ctx, buf, n), "sd_phase_trace_read")
+        self._waited(B.sd_phase_trace_read(self.ctx, buf, n), "sd_phase_trace_read")
         ent = buf[:n.value]
         if len(ent) == 0:
             return []
@@ -316,15 +324,14 @@ class Session:
     def guard_read(self):
         """Record of a -DSDFP_GUARD build: (violations, [(site, address, bytes, workgroup, thread)])."""
         buf = np.zeros(32, np.uint64)
-        self._check(B.sd_guard_read(self.ctx, buf), "sd_guard_read")
+        self._waited(B.sd_guard_read(self.ctx, buf), "sd_guard_read")
         n = int(buf[0])
         recs = [(int(buf[1 + 3 * i]), hex(int(buf[2 + 3 * i])), int(buf[3 + 3 * i]) & 0xFFFFFFFF,
                  (int(buf[3 + 3 * i]) >> 32) & 0xFFFF, int(buf[3 + 3 * i]) >> 48) for i in range(min(n, 10))]
         return n, recs
 
     def sync(self):
-        self._check(B.sd_sync(self.ctx), "sd_sync")
-        self._retired.clear()
+        self._waited(B.sd_sync(self.ctx), "sd_sync")
 
     def read(self, cap: Optional[int] = None):
         """Returns (tokens int32[n], stats dict).  Waits for the stream."""
@@ -332,13 +339,13 @@ class Session:
         buf = np.zeros(cap, np.int32)
         n = ctypes.c_int32(0)
         st = B.SdStats()
-        self._check(B.sd_read(self.ctx, buf, n, st), "sd_read")
+        self._waited(B.sd_read(self.ctx, buf, n, st), "sd_read")
         stats = {k: getattr(st, k) for k, _ in B.SdStats._fields_}
         return buf[:min(n.value, cap)].copy(), stats
 
     def committed(self) -> int:
         n = ctypes.c_int32(0)
-        self._check(B.sd_read(self.ctx, None, n, None), "sd_read")
+        self._waited(B.sd_read(self.ctx, None, n, None), "sd_read")
         return n.value
 
     def dump_logits(self, which, rows):
@@ -349,7 +356,7 @@ class Session:
 
     def dump_draft(self, K):
         out = np.zeros(max(K, 1), np.int32)
-        self._check(B.sd_dump_draft(self.ctx, out), "sd_dump_draft")
+        self._waited(B.sd_dump_draft(self.ctx, out), "sd_dump_draft")
         return out[:K]
 
     # ---- outer loops ------------------------------------------------------------------------------------
