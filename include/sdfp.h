@@ -290,7 +290,8 @@ int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_
  * of the grid 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign.  A matrix of rows x cols lies in panels of 64 rows x 128 columns,
  * [ceil(rows / 64)][ceil(cols / 128)][4352 bytes]: 4096 bytes of codes -- row 16 t + r, block b of the panel at
  * ((t * 4 + b) * 16 + r) * 16, column 2 i of the block in the low four bits of byte i, column 2 i + 1 in the high four --,
- * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes.  A scale byte 255 marks a block of NaN
+ * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes; the scale bytes of blocks
+ * that lie wholly past it may be anything.  A scale byte 255 marks a block of NaN
  * (0 stands for 2^-127; what float32 cannot hold, 6 * 2^127, becomes an infinity).
  * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned.  A matrix that is
  * quantised, read back or multiplied has fewer than 2^24 panels. */

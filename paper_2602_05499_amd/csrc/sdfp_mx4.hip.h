@@ -3,6 +3,8 @@
 #include "sdfp_common.hip.h"
 #include "sdfp_mx4.h"
 
+#include <type_traits>
+
 namespace sdfp {
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // 16 bytes at any element's address
@@ -195,6 +197,12 @@ __device__ __forceinline__ f32x4 mx4_mfma(const u32x4& a, int sa, const u32x4& b
 }
 // the high bit of every byte of s that is 255
 __device__ __forceinline__ unsigned mx4_nan_bytes(unsigned s) { return ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u; }
+
+// A lane's word of scales in the last panel.  Blocks past column K hold zero codes, but any scale byte: theirs become 0, so that a 255
+// there counts for nothing.
+__device__ __forceinline__ unsigned mx4_last_scales(unsigned s, int lane, int kps, int K) {
+    return (kps - 1) * MX4_COLS + lane / 16 * MX4_BLOCK < K ? s : 0u;
+}
 
 // four neighbouring outputs n .. n + 3 of row m (those that exist)
 __device__ __forceinline__ void mx4_store(const Mx4Product& a, int64_t m, int64_t n, const float (&v)[4]) {
@@ -417,17 +425,31 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
             __builtin_amdgcn_sched_barrier(0);
             fetch(kp + 3 * W, aft, false);
         }
-        if (kp < full) multiply(nxt);
+        auto finish = [&](int p, Load& L) {
+            if (p >= full) return;
+            if (p == full - 1) {
+#pragma unroll
+                for (int q = 0; q < NPAN; ++q) L.scale[q] = mx4_last_scales(L.scale[q], lane, kps, a.K);
+                L.gain.x = mx4_last_scales(L.gain.x, lane, kps, a.K);
+            }
+            multiply(L);
+        };
+        finish(kp, nxt);
         if (kp + 2 * W < full) fetch(kp + 2 * W, nxt, false);
-        if (kp + W < full) multiply(aft);
-        if (kp + 2 * W < full) multiply(nxt);
+        finish(kp + W, aft);
+        finish(kp + 2 * W, nxt);
     } else {
         for (int kp = wave; kp < full; kp += W) {
             const Load cur = nxt;
             fetch(min(kp + W, full - 1), nxt, false);
             multiply(cur);
         }
-        if (full < kps && full % W == wave) { fetch(full, nxt, true); multiply(nxt); }
+        if (full < kps && full % W == wave) {
+            fetch(full, nxt, true);
+#pragma unroll
+            for (int q = 0; q < NPAN; ++q) nxt.scale[q] = mx4_last_scales(nxt.scale[q], lane, kps, a.K);
+            multiply(nxt);
+        }
     }
 
     // the waves' sums, in wave order (and the pieces' after one another), a panel at a time
@@ -656,6 +678,7 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
         fetch(full, f0, false);
         store_x(f0, sh, true);
         __syncthreads();
+        if (full * KW + kg == kps - 1) f0.scale = mx4_last_scales(f0.scale, lane, kps, a.K);
         if (full * KW + kg < kps) multiply(sh, f0, [] {});
         __syncthreads();
     }
@@ -780,8 +803,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
         for (int i = 0; i < S::NT; ++i) *reinterpret_cast<u32x4*>(buf + (wave * S::NT + i) * MX4_TILE_BYTES + lane * 16) = f.x[i];
         *reinterpret_cast<unsigned*>(buf + S::XP * MX4_CODE_BYTES + s_at * 4) = f.sx;
     };
-    // step st: the tiles of x lie in LDS, the rest in f; next's tiles go to LDS
-    auto step = [&](int st, Load& f, const Load& next) {
+    // step st: the tiles of x lie in LDS, the rest in f; next's tiles go to LDS (more: there is a next step)
+    auto step = [&](int st, Load& f, const Load& next, auto more) {
         const char* px = sh + (st & 1) * S::BUF + wm * CT * MX4_TILE_BYTES + lane * 16;
         const char* ps = sh + (st & 1) * S::BUF + S::XP * MX4_CODE_BYTES + wm * CT * 64 + lane * 4;
         unsigned sx[CT / 4];
@@ -790,7 +813,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
         for (int i = 0; i < CT / 4; ++i) sx[i] = *reinterpret_cast<const unsigned*>(ps + i * 256);
 #pragma unroll
         for (int c = 0; c < CT; ++c) x[c] = *reinterpret_cast<const u32x4*>(px + c * MX4_TILE_BYTES);
-        fetch_x(st + 2, f);
+        if (more) fetch_x(st + 2, f);
         bad |= mx4_nan_bytes(f.sw);
 #pragma unroll
         for (int i = 0; i < CT / 4; ++i) bad_x[i] |= mx4_nan_bytes(sx[i]);
@@ -799,10 +822,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
 #pragma unroll
             for (int c = 0; c < CT; ++c) acc[t][c] = mx4_mfma(f.w[t], (int)(f.sw >> (8 * t)), x[c], (int)(sx[c / 4] >> (8 * (c % 4))), acc[t][c]);
             __builtin_amdgcn_sched_barrier(0);
-            fetch_w(st + 2, t, f);
+            if (more) fetch_w(st + 2, t, f);
         }
-        fetch_s(st + 2, f);
-        store(next, sh + (~st & 1) * S::BUF);
+        if (more) {
+            fetch_s(st + 2, f);
+            store(next, sh + (~st & 1) * S::BUF);
+        }
         __syncthreads();
     };
     auto fetch = [&](int st, Load& f) {
@@ -815,9 +840,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_mx4_tiles_mx4(Mx4Product a)
     fetch(1, f1);
     store(f0, sh);
     __syncthreads();
+    const int last = kps - 1;
     int st = 0;
-    for (; st + 1 < kps; st += 2) { step(st, f0, f1); step(st + 1, f1, f0); }
-    if (st < kps) step(st, f0, f1);
+    for (; st + 1 < last; st += 2) { step(st, f0, f1, std::true_type()); step(st + 1, f1, f0, std::true_type()); }
+    if (st < last) { step(st, f0, f1, std::true_type()); f0 = f1; }
+    if (last * MX4_COLS + 3 * MX4_BLOCK >= a.K) {   // blocks past the matrix: the last step by itself (their test in the loop: 1024 x 4096 x 14336 46 -> 50 us)
+        f0.sw = mx4_last_scales(f0.sw, lane, kps, a.K);
+        unsigned* sx = reinterpret_cast<unsigned*>(sh + (last & 1) * S::BUF + S::XP * MX4_CODE_BYTES + s_at * 4);
+        *sx = mx4_last_scales(*sx, s_at % 64, kps, a.K);
+        __syncthreads();
+    }
+    step(last, f0, f0, std::false_type());
     unsigned nan[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
