@@ -291,8 +291,9 @@ int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_
  * [ceil(rows / 64)][ceil(cols / 128)][4352 bytes]: 4096 bytes of codes -- row 16 t + r, block b of the panel at
  * ((t * 4 + b) * 16 + r) * 16, column 2 i of the block in the low four bits of byte i, column 2 i + 1 in the high four --,
  * then its scale bytes at 4096 + (b * 16 + r) * 4 + t.  Rows and columns past the matrix hold zero codes; the scale bytes of blocks
- * that lie wholly past it may be anything.  A scale byte 255 marks a block of NaN
- * (0 stands for 2^-127; what float32 cannot hold, 6 * 2^127, becomes an infinity).
+ * that lie wholly past it may be anything.  A scale byte 255 marks a block of NaN (0 stands for 2^-127; what float32 cannot
+ * hold -- 2, 3, 4 and 6 * 2^127, 4 and 6 * 2^126 -- is read back, and multiplied with rows of x, as an infinity; a product with
+ * both sides in MXFP4 takes the value itself, and only its sum is held to float32's range).
  * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned.  A matrix that is
  * quantised, read back or multiplied has fewer than 2^24 panels. */
 size_t sd_mx4_bytes(int32_t rows, int32_t cols);

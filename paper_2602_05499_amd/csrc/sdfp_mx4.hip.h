@@ -198,6 +198,35 @@ __device__ __forceinline__ f32x4 mx4_mfma(const u32x4& a, int sa, const u32x4& b
 // the high bit of every byte of s that is 255
 __device__ __forceinline__ unsigned mx4_nan_bytes(unsigned s) { return ((s & 0x7F7F7F7Fu) + 0x01010101u) & s & 0x80808080u; }
 
+// The same for bytes from 253 on, whose larger values pass float32.  Where float32 x has its three pieces in one sum, an infinity among
+// w's values multiplies all three and makes NaN of the pieces that are zero; outputs whose row of w has such a byte (or a 255) are
+// therefore added up again, one thread each.
+__device__ __forceinline__ unsigned mx4_far_bytes(unsigned s) { return ((s & 0x7F7F7F7Fu) + 0x03030303u) & s & 0x80808080u; }
+// Output (m, n): NaN with a block of NaN, y if w's values are all finite, else the sum of the terms that are not finite.  rs: the row's
+// factor.
+__device__ __forceinline__ float mx4_far_output(const Mx4Product& a, int64_t m, int64_t n, float rs, float y) {
+    const int kps = (a.K + MX4_COLS - 1) / MX4_COLS, t = (int)(n % MX4_ROWS) / 16, r = (int)(n % 16);
+    const char* w = a.w + (size_t)(n / MX4_ROWS) * kps * MX4_PANEL_BYTES;
+    auto block = [&](int k) { return k % MX4_COLS / MX4_BLOCK * 16 + r; };
+    auto scale = [&](int k) { return (int)(unsigned char)w[(size_t)(k / MX4_COLS) * MX4_PANEL_BYTES + MX4_CODE_BYTES + block(k) * 4 + t]; };
+#pragma unroll 1
+    for (int k = 0; k < a.K; k += MX4_BLOCK)
+        if (scale(k) == 255) return __uint_as_float(0x7FC00000u);
+    const float* x = (const float*)a.x + m * a.ldx;
+    bool inf = false;
+    float sum = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < a.K; ++k) {
+        const int e = scale(k);
+        const int code = (unsigned char)w[(size_t)(k / MX4_COLS) * MX4_PANEL_BYTES + t * MX4_TILE_BYTES + block(k) * 16 + k % MX4_BLOCK / 2] >> (4 * (k % 2)) & 15;
+        const bool far = (code & 7) >= (e == 254 ? 4 : e == 253 ? 6 : 8);          // 2 * 2^127, 4 * 2^126
+        const float v = a.gain ? x[k] * a.gain[k] : x[k], c = far ? INFINITY : code & 7 ? 1.f : 0.f;
+        if (far || !__builtin_isfinite(v)) sum += v * (code & 8 ? -c : c);
+        inf |= far;
+    }
+    return inf ? sum * rs : y;
+}
+
 // A lane's word of scales in the last panel.  Blocks past column K hold zero codes, but any scale byte: theirs become 0, so that a 255
 // there counts for nothing.
 __device__ __forceinline__ unsigned mx4_last_scales(unsigned s, int lane, int kps, int K) {
@@ -276,6 +305,7 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
     constexpr bool COLS = mx4_rows_in_columns(XT, MP);
     constexpr int NPC = XT == MX4_X_F32 ? 3 : 1;                             // pieces of a value
     constexpr int NI = COLS ? 1 : NPC;                                       // instructions per sub-step and tile
+    constexpr bool FAR = XT == MX4_X_F32 && !COLS;                           // s_bad_n: outputs to be added up again (else: NaN)
     // the staged panel of x, one piece after the other (or with the pieces as columns): 16 entries -- sub-step j, block b -- of
     // 16 bytes per column, a multiple of 16 bytes apart that is no power of two, so that the lanes of a row write to different
     // banks
@@ -388,7 +418,7 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
             }
 #pragma unroll
             for (int q = 0; q < NPAN; ++q) {
-                bad[q] |= mx4_nan_bytes(L.scale[q]);
+                bad[q] |= FAR ? mx4_far_bytes(L.scale[q]) : mx4_nan_bytes(L.scale[q]);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
                     const unsigned e = L.scale[q] >> (8 * t) & 255u;
@@ -481,27 +511,48 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
         const int nr = (tid >> 6) * 16 + g * 4;
         const int64_t n = (int64_t)(panel0 + q) * MX4_ROWS + t0 * 16 + nr;
         if (tid >= TT * 64 || c16 >= MP || m >= a.M || n >= a.N) continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, first[4], rs = 1.f;
 #pragma unroll
-        for (int p = 0; p < (COLS ? 3 : 1); ++p)
+        for (int p = 0; p < (COLS ? 3 : 1); ++p) {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const f32x4 o = *reinterpret_cast<const f32x4*>(sh + (w * TT * 64 + tid + p * MP) * 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] += o[i];
             }
+            if (p == 0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) first[i] = v[i];
+        }
+        if (COLS)       // an infinity of w times a zero second or third piece is NaN: the first piece alone has IEEE's result
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] == v[i] ? v[i] : first[i];
         if constexpr (XT == MX4_X_F32)
             if (a.gain) {
                 float ss = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) ss += s_sq[w][c16];
-                const float rs = rms_recip(ss, a.K, a.eps);
+                rs = rms_recip(ss, a.K, a.eps);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] *= rs;
             }
+        if constexpr (FAR) {
+            unsigned again = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (s_bad_n[q * MX4_ROWS + nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
+            for (int i = 0; i < 4; ++i) again |= n + i < a.N ? s_bad_n[q * MX4_ROWS + nr + i] << i : 0u;
+            if (__builtin_expect(again != 0u, 0))
+#pragma unroll 1
+                for (; again; again &= again - 1) {
+                    const int at = __builtin_ctz(again);
+                    const float y = mx4_far_output(a, m, n + at, rs, at == 0 ? v[0] : at == 1 ? v[1] : at == 2 ? v[2] : v[3]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = i == at ? y : v[i];
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s_bad_n[q * MX4_ROWS + nr + i] | s_bad_m[c16]) v[i] = __uint_as_float(0x7FC00000u);
+        }
         mx4_store(a, m, n, v);
     }
 }
@@ -618,7 +669,7 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
     // decoded: called when the codes in f are not needed any more
     auto multiply = [&](const char* buf, Load& f, auto decoded) {
         buf += kg * S::PANEL + wm * CT * 4096 + lane * 16;
-        bad |= mx4_nan_bytes(f.scale);
+        bad |= XT == MX4_X_F32 ? mx4_far_bytes(f.scale) : mx4_nan_bytes(f.scale);
         float s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -718,9 +769,9 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
     } else if (XT == MX4_X_F32 && a.gain) {
         __syncthreads();
     }
-    unsigned nan[4];
+    unsigned odd = 0;               // bit 4 t + i: that output of the lane is NaN, or (float32) to be added up again
 #pragma unroll
-    for (int t = 0; t < 4; ++t) nan[t] = mx4_nan_rows(bad, t) >> (g * 4);
+    for (int t = 0; t < 4; ++t) odd |= (mx4_nan_rows(bad, t) >> (g * 4) & 15u) << (4 * t);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const int mr = (wm * CT + c) * 16;
@@ -739,7 +790,20 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
             for (int i = 0; i < 4; ++i) {
                 v[t][i] = acc[t][c][i];
                 if (XT == MX4_X_F32 && a.gain) v[t][i] *= rs;
-                if (nan[t] >> i & 1u) v[t][i] = __uint_as_float(0x7FC00000u);
+                if (XT != MX4_X_F32 && odd >> (4 * t + i) & 1u) v[t][i] = __uint_as_float(0x7FC00000u);
+            }
+        if (XT == MX4_X_F32 && __builtin_expect(odd != 0u, 0))
+#pragma unroll 1
+            for (unsigned left = odd; left; left &= left - 1) {
+                const int at = __builtin_ctz(left);
+                const int64_t m = m0 + mr + c16, n = (int64_t)panel * MX4_ROWS + at / 4 * 16 + g * 4 + at % 4;
+                if (m >= a.M || n >= a.N) continue;
+                float y = 0.f;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) y = k == at ? v[k / 4][k % 4] : y;
+                y = mx4_far_output(a, m, n, rs, y);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k / 4][k % 4] = k == at ? y : v[k / 4][k % 4];
             }
         mx4_store_tile(a, sh + S::RED + wave * MX4_OUT_BYTES, m0 + mr, (int64_t)panel * MX4_ROWS, v);
     }
