@@ -1326,7 +1326,7 @@ int sd_set_rules(sd_ctx* c, const sd_rules* rules, const int32_t* next, int32_t 
     const int start_before = c->rules_start;
     c->rules = r;
     c->rules_start = rules->allowed ? state : -1;
-    if (r.r.allowed) hipLaunchKernelGGL(k_rules_usable, dim3((unsigned)r.r.n_masks), dim3(256), 0, c->stream, r.r.allowed, c->cfg.vocab, usable);
+    if (r.r.allowed) hipLaunchKernelGGL(k_rules_usable, dim3(std::min(r.r.n_masks, RULES_MASK_GRID)), dim3(256), 0, c->stream, r.r.allowed, r.r.n_masks, c->cfg.vocab, usable);
     if (c->phase == PH_READY) rules_begin(c, true);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) {   // nothing was set up: the context keeps what it had

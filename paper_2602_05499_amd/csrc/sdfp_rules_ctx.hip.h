@@ -21,14 +21,18 @@ __device__ __forceinline__ int rules_step(const CtxRules& c, int s, int tok, int
     const int n = c.next[(int64_t)s * V + tok];
     return n >= 0 && n < c.r.n_masks ? n : -1;
 }
-// usable[m]: mask m allows some token of the vocabulary.  One workgroup per mask.
-__global__ __launch_bounds__(256) void k_rules_usable(const unsigned* __restrict__ allowed, int V, int* __restrict__ usable) {
+// usable[m]: mask m allows some token of the vocabulary.  A workgroup per mask, up to RULES_MASK_GRID of them (a launch does not
+// hold one for each of 2^24 masks).
+constexpr int RULES_MASK_GRID = 65536;
+__global__ __launch_bounds__(256) void k_rules_usable(const unsigned* __restrict__ allowed, int n_masks, int V, int* __restrict__ usable) {
     const int words = (V + 31) / 32;
-    const unsigned* m = allowed + (int64_t)blockIdx.x * words;
-    unsigned any = 0;
-    for (int w = threadIdx.x; w < words; w += 256) any |= w == words - 1 && V % 32 ? m[w] & ((1u << (V % 32)) - 1u) : m[w];
-    const int r = __syncthreads_or(any != 0u);
-    if (threadIdx.x == 0) usable[blockIdx.x] = r ? 1 : 0;
+    for (int64_t i = blockIdx.x; i < n_masks; i += gridDim.x) {
+        const unsigned* m = allowed + i * words;
+        unsigned any = 0;
+        for (int w = threadIdx.x; w < words; w += 256) any |= w == words - 1 && V % 32 ? m[w] & ((1u << (V % 32)) - 1u) : m[w];
+        const int r = __syncthreads_or(any != 0u);
+        if (threadIdx.x == 0) usable[i] = r ? 1 : 0;
+    }
 }
 // counts (cleared before) += the prompt and, unless the sequence is new, the committed tokens; the start state
 __global__ __launch_bounds__(256) void k_rules_history(CtxRules c, int V, int start, const int* __restrict__ prompt, int n_prompt,
