@@ -295,7 +295,8 @@ int sd_fit_prune_sublayers(const double *t_attn, const double *t_ffn, int32_t n_
  * hold -- 2, 3, 4 and 6 * 2^127, 4 and 6 * 2^126 -- is read back, and multiplied with rows of x, as an infinity; a product with
  * both sides in MXFP4 takes the value itself, and only its sum is held to float32's range).
  * sd_mx4_bytes: bytes of a matrix (0 if a size is not positive).  A buffer of panels is 256-byte aligned.  A matrix that is
- * quantised, read back or multiplied has fewer than 2^24 panels. */
+ * quantised, read back or multiplied has fewer than 2^24 panels; besides, a product has fewer than 2^23 times 64 outputs per row
+ * if it has up to 16 rows, and fewer than 2^23 tiles of 64 rows by 256 outputs if it has more (else SD_EINVAL). */
 size_t sd_mx4_bytes(int32_t rows, int32_t cols);
 /* Quantise rows (dtype SD_F32 or SD_BF16, ld >= cols elements apart, any alignment of their elements): the scale of a block
  * is 2^(floor(log2 max|x|) - 2), at least 2^-126, and every value is rounded to the nearest grid value (ties to the even
