@@ -81,7 +81,12 @@ static hipError_t launch_tiles_mx4(const Mx4Product& a, hipStream_t s) {
 //             4096 x 14336 866/757/421/351 (1.37 PFLOP/s; the library's bfloat16 product of that size 396)
 //   float32   128 x 4096 23/46/49/121, 512 x 4096 70/52/54/121, 256 x 11008 95/90/78/120, 2048 x 4096 249/181/162/134,
 //             4096 x 14336 1786/1256/1111/935 (three products: 1.54 PFLOP/s)
-//   MXFP4     128 x 4096 13/14/-/22, 256 x 11008 32/18/-/23, 2048 x 4096 65/26/-/26, 4096 x 14336 442/201/-/150 (3.2 PFLOP/s)
+//   MXFP4     128 x 4096 13/14/-/23, 64 x 11008 16/14/-/22, 256 x 11008 32/19/-/24, 2048 x 4096 66/28/-/27, 4096 x 14336 522/196/-/150 (3.2
+//             PFLOP/s)
+// K does not enter: over 14 sizes from 16 x 4096 to 4096 x 14336 the choice is within 7 % of the best at K 512, 4096 and 14336, but for
+// float32 (K 512: 64 x 11008 12.7 against 10.7 by the middle tile, 512 x 4096 13.0 against 11.8; K 14336: 256 x 4096 118 against 108 by
+// few rows, 512 x 4096 176 against 161 by the small tile, 1024 x 4096 307 against 286 by the middle one) and for 2048 x 4096 x 512 in
+// MXFP4 (12.0 against 11.1 by the small tile).
 hipError_t mx4_product(const Mx4Product& a, hipStream_t stream) {
     const int64_t n_pan = mx4_row_panels(a.N), pieces = n_pan * (((int64_t)a.M + 15) / 16);
     auto tiles = [&](int n, int m) { return (((int64_t)a.N + n - 1) / n) * (((int64_t)a.M + m - 1) / m); };

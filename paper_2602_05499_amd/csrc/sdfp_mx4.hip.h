@@ -291,7 +291,7 @@ __device__ __forceinline__ void mx4_store_tile(const Mx4Product& a, char* lds, i
 // with the launch's ends; 128256 x 4096 46.5 us, 6.0 TB/s; x in MXFP4 5 rows 43.3 us, 6.5 TB/s).  A workgroup computes NPAN panels of outputs, or TT of the four 16-row tiles of one,
 // for 16 rows of x; its waves split the reduction dimension by panels and add their sums in wave order at the end.  The codes
 // go from memory straight into the A operand (lane l: weight row l % 16, the block l / 16 of 32 columns; sub-step j multiplies
-// the 8 values of word j), one panel ahead, x through a few kilobytes of LDS
+// the 8 values of word j), one panel ahead (x in MXFP4: two), x through a few kilobytes of LDS
 // that belong to the wave into the B operand, in the same order of columns.  x in MXFP4 goes as it is into the scaled 4-bit
 // instruction; float32 x is cut into three exact bfloat16 pieces, which take three of the operand's 16 columns for each row
 // while rows are few (MP <= 5: one instruction where three would run, 17.7 -> 15.5 us) and three instructions otherwise.  MP:
@@ -435,8 +435,8 @@ __global__ __launch_bounds__(MX4_WAVES * 64) void k_mx4_rows(Mx4Product a) {
     };
 
     const int full = XT == MX4_X_MX4 ? kps : a.K / MX4_COLS;                 // panels without a ragged end
-    // Every load of the loops is unconditional (past the end the last panel once more): behind a load under a condition the
-    // compiler waits for everything in flight, the panel ahead included.
+    // Every load inside the loops is unconditional (x in rows: past the end the last panel once more; x in MXFP4: the loop ends before
+    // that): behind a load under a condition the compiler waits for everything in flight, the panel ahead included.
     Load nxt;
     if (wave < full) fetch(wave, nxt, false);
     for (int i = tid; i < NPAN * MX4_ROWS; i += W * 64) s_bad_n[i] = 0;
@@ -814,8 +814,9 @@ __global__ __launch_bounds__(64 * WN * WM * KW, 2) void k_mx4_tiles(Mx4Product a
 // through LDS (two buffers), a wave's panel of w straight into its registers, everything two steps of 128 columns ahead: with w
 // in LDS as well its bandwidth was the bound, and scales of x that every wave loads for itself wait for one another (1024 rows x
 // 4096 x 14336: 44 us, those loads 50).  4096 rows x 14336 x 4096 at 3.2 PFLOP/s, 4096 x 4096 x 14336 at 4.3, of the 8.0 that these
-// instructions reach without loads; of the former's 150 us 42 are the write of 235 MB of float32 results, which nothing hides
-// (workgroups started at different times: the same).
+// instructions reach without loads.  Of the former's 150 us 42 go with the write of 235 MB of float32 results, which a workgroup does
+// at its end with nothing else in flight (workgroups started at different times: the same), and its 1792 tiles are three and a half
+// rounds of the two workgroups that a compute unit holds.
 template <int CT, int WN, int WM>
 struct Mx4TileX {
     static constexpr int WAVES = WN * WM, XP = CT * WM / 4, BUF = XP * MX4_PANEL_BYTES;   // all tiles of x, then their scales
