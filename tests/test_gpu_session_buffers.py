@@ -31,6 +31,7 @@ WAITS = {
 @pytest.mark.parametrize("which", list(WAITS))
 def test_replaced_tensors_are_let_go(P, which):
     """A grammar and a head for every request, as many as there are requests: the memory stays that of one of them."""
+    import gc
     import torch
     s = _shape("bf16", 2050)
     dw = _weights(s, synth.gen_skip_mask(s))
@@ -39,6 +40,7 @@ def test_replaced_tensors_are_let_go(P, which):
     ses = P.Session(s, dw, synth.gen_skip_mask(s), max_seq=96, max_k=4)
     ses.prefill(prompt)
     held = []
+    gc.collect()                                         # what earlier tests left behind
     for i in range(7):
         ses.set_rules(**{k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in dev.items()})
         ses.set_draft_head(P.mx4_quantize(dw.lm_head))
